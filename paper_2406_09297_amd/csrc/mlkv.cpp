@@ -15,21 +15,8 @@
 
 #include <rocblas/rocblas.h>
 
+#include "host.h"
 #include "kernels.h"
-
-struct mlkv_map {
-  int l = 0, h = 0, n_kv = 0;
-  std::vector<int32_t> kv_of;     // [l*h]
-  std::vector<int32_t> owner_of;  // [n_kv]
-  // per layer: the KV heads read form [kv_begin, kv_begin + kv_count), G = h / kv_count
-  std::vector<int> kv_begin, kv_count, group;
-  // per layer: the KV heads appended form [own_begin, own_begin + own_count)
-  std::vector<int> own_begin, own_count;
-  // > 0: the layers fall into groups of this many consecutive layers, each
-  // reading the same number of KV heads, its own, which its first layer
-  // appends (every uniform map): a decode step may take all layers at once.
-  int layers_per_group = 0;
-};
 
 struct mlkv_model {
   const mlkv_map* map = nullptr;
@@ -46,10 +33,13 @@ struct mlkv_model {
 };
 
 namespace {
-
 thread_local std::string g_last_error;
+constexpr int kFallbackResident = 768;  // 256 CUs x 3 when no device can be queried
+}  // namespace
 
-mlkv_status fail(mlkv_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace mlkv {
+namespace host {
+
 mlkv_status fail(mlkv_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -65,10 +55,74 @@ mlkv_status ok() {
   return MLKV_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+thread_local Profile g_profile;
 
-constexpr int kTileTokens = 32;
+mlkv_status check_map(const mlkv_map* map) {
+  if (!map) return fail(MLKV_ERR_INVALID_ARG, "map is NULL");
+  return MLKV_OK;
+}
+
+mlkv_status check_cache(const mlkv_cache* c, const mlkv_map* map) {
+  if (!c) return fail(MLKV_ERR_INVALID_ARG, "cache is NULL");
+  if (!c->k || !c->v) return fail(MLKV_ERR_INVALID_ARG, "cache planes must be non-NULL");
+  if (!aligned16(c->k) || !aligned16(c->v))
+    return fail(MLKV_ERR_ALIGNMENT, "cache planes must be 16-byte aligned");
+  if (c->batch <= 0 || c->capacity <= 0)
+    return fail(MLKV_ERR_INVALID_ARG, "cache batch and capacity must be positive");
+  if (c->capacity % kTileTokens != 0)
+    return fail(MLKV_ERR_CAPACITY, "cache capacity %d is not a multiple of 32", c->capacity);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(MLKV_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", c->head_dim);
+  if (c->n_kv != map->n_kv)
+    return fail(MLKV_ERR_INVALID_ARG, "cache has %d KV heads, map has %d", c->n_kv, map->n_kv);
+  const double elems = 2.0 * c->n_kv * c->batch * static_cast<double>(c->capacity) * c->head_dim;
+  if (elems > 9.0e18) return fail(MLKV_ERR_CAPACITY, "cache too large");
+  return MLKV_OK;
+}
+
+long compute_units_or_fallback() {
+  const long cus = mlkv::compute_units();
+  return cus > 0 ? cus : kFallbackResident / 3;
+}
+
+mlkv_status check_lengths_if_requested(const int32_t* lens, int batch, int offset, int limit,
+                                       hipStream_t stream) {
+  const char* env = std::getenv("MLKV_CHECK");
+  if (!env || std::strcmp(env, "1") != 0) return MLKV_OK;
+  std::vector<int32_t> host(batch);
+  if (hipStreamSynchronize(stream) != hipSuccess ||
+      hipMemcpy(host.data(), lens, sizeof(int32_t) * batch, hipMemcpyDeviceToHost) != hipSuccess)
+    return fail(MLKV_ERR_HIP, "MLKV_CHECK: could not read lengths back");
+  for (int b = 0; b < batch; ++b) {
+    const long L = static_cast<long>(host[b]) + offset;
+    if (L < 0 || L > limit)
+      return fail(MLKV_ERR_CAPACITY, "MLKV_CHECK: sequence %d attends %ld positions, limit %d", b,
+                  L, limit);
+  }
+  return MLKV_OK;
+}
+
+mlkv_status check_prefill_lengths_if_requested(const int32_t* ctx, int batch, int T, int S,
+                                               hipStream_t stream) {
+  const char* env = std::getenv("MLKV_CHECK");
+  if (!env || std::strcmp(env, "1") != 0) return MLKV_OK;
+  std::vector<int32_t> host(batch);
+  if (hipStreamSynchronize(stream) != hipSuccess ||
+      hipMemcpy(host.data(), ctx, sizeof(int32_t) * batch, hipMemcpyDeviceToHost) != hipSuccess)
+    return fail(MLKV_ERR_HIP, "MLKV_CHECK: could not read lengths back");
+  for (int b = 0; b < batch; ++b)
+    if (host[b] < 0 || static_cast<long>(host[b]) + T > S)
+      return fail(MLKV_ERR_CAPACITY, "MLKV_CHECK: sequence %d has %d cached + %d new tokens, "
+                  "capacity %d", b, host[b], T, S);
+  return MLKV_OK;
+}
+
+}  // namespace host
+}  // namespace mlkv
+
+using namespace mlkv::host;
+
+namespace {
 
 // Derive the per-layer structure of a map; returns an error message or "".
 std::string analyse(mlkv_map& m) {
@@ -128,33 +182,6 @@ std::string analyse(mlkv_map& m) {
   return "";
 }
 
-mlkv_status check_map(const mlkv_map* map) {
-  if (!map) return fail(MLKV_ERR_INVALID_ARG, "map is NULL");
-  return MLKV_OK;
-}
-
-mlkv_status check_cache(const mlkv_cache* c, const mlkv_map* map) {
-  if (!c) return fail(MLKV_ERR_INVALID_ARG, "cache is NULL");
-  if (!c->k || !c->v) return fail(MLKV_ERR_INVALID_ARG, "cache planes must be non-NULL");
-  if (!aligned16(c->k) || !aligned16(c->v))
-    return fail(MLKV_ERR_ALIGNMENT, "cache planes must be 16-byte aligned");
-  if (c->batch <= 0 || c->capacity <= 0)
-    return fail(MLKV_ERR_INVALID_ARG, "cache batch and capacity must be positive");
-  if (c->capacity % kTileTokens != 0)
-    return fail(MLKV_ERR_CAPACITY, "cache capacity %d is not a multiple of 32", c->capacity);
-  if (c->head_dim != 64 && c->head_dim != 128)
-    return fail(MLKV_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", c->head_dim);
-  if (c->n_kv != map->n_kv)
-    return fail(MLKV_ERR_INVALID_ARG, "cache has %d KV heads, map has %d", c->n_kv, map->n_kv);
-  const double elems = 2.0 * c->n_kv * c->batch * static_cast<double>(c->capacity) * c->head_dim;
-  if (elems > 9.0e18) return fail(MLKV_ERR_CAPACITY, "cache too large");
-  return MLKV_OK;
-}
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-int tiles_of(int len) { return (len + kTileTokens - 1) / kTileTokens; }
-
 // Split-K plan for one layer.  The kernel cuts every (sequence, KV head)
 // unit into runs of R tiles, R chosen on the device from the actual lengths
 // so that all runs fit the launched workgroups.  The host picks that count:
@@ -181,17 +208,10 @@ struct Plan {
 constexpr int kMinTiles = 8;
 constexpr int kSingleUnitTiles = 16;
 constexpr int kMaxRunsPerUnit = 128;
-constexpr long kCounterSlots = 65536;  // arrival counters of a workspace
 // Launches that schedule their runs on the device use at most this many
 // workgroups (the schedule counts runs in 16-bit halves).
 constexpr long kMaxScheduledWorkgroups = 16384;
-constexpr int kFallbackResident = 768;  // 256 CUs x 3 when no device can be queried
 constexpr int kWorkgroupsPerCu = 2;
-
-long compute_units_or_fallback() {
-  const long cus = mlkv::compute_units();
-  return cus > 0 ? cus : kFallbackResident / 3;
-}
 
 long workgroups_for(long resident, long units, long t_max, int min_tiles) {
   long g = resident < kMaxRunsPerUnit * units ? resident : kMaxRunsPerUnit * units;
@@ -491,31 +511,6 @@ size_t workspace_need(int batch, int h, int head_dim, const Plan& pl) {
   return ws_layout(batch, h, head_dim, pl).total;
 }
 
-mlkv_status check_lengths_if_requested(const int32_t* lens, int batch, int offset, int limit,
-                                       hipStream_t stream) {
-  const char* env = std::getenv("MLKV_CHECK");
-  if (!env || std::strcmp(env, "1") != 0) return MLKV_OK;
-  std::vector<int32_t> host(batch);
-  if (hipStreamSynchronize(stream) != hipSuccess ||
-      hipMemcpy(host.data(), lens, sizeof(int32_t) * batch, hipMemcpyDeviceToHost) != hipSuccess)
-    return fail(MLKV_ERR_HIP, "MLKV_CHECK: could not read lengths back");
-  for (int b = 0; b < batch; ++b) {
-    const long L = static_cast<long>(host[b]) + offset;
-    if (L < 0 || L > limit)
-      return fail(MLKV_ERR_CAPACITY, "MLKV_CHECK: sequence %d attends %ld positions, limit %d", b,
-                  L, limit);
-  }
-  return MLKV_OK;
-}
-
-// Event pairs around attention launches (mlkv_profile_*).
-struct Profile {
-  std::vector<hipEvent_t> start, stop;
-  int used = 0;
-  bool on = false;
-};
-thread_local Profile g_profile;
-
 // plan_mode: 0 = every workgroup schedules inside the attention kernel;
 // 1 = the same, and each workgroup also records its run in the workspace's
 // plan; 2 = follow the plan already recorded there (same lengths and launch).
@@ -644,7 +639,6 @@ mlkv_status append_rows_impl(int kv_begin, int owned, const mlkv_cache* cache, c
 
 // Prefill shape checks shared by the entry points: 0 <= T <= capacity and the
 // launch grid within its limits for every layer.
-constexpr long kMaxGridY = 65535;
 mlkv_status check_prefill_shape(const mlkv_map* map, const mlkv_cache* cache, int T) {
   if (T < 0 || T > cache->capacity)
     return fail(MLKV_ERR_CAPACITY, "T = %d new tokens: must be in [0, capacity %d]", T,
@@ -656,22 +650,6 @@ mlkv_status check_prefill_shape(const mlkv_map* map, const mlkv_cache* cache, in
       return fail(MLKV_ERR_UNSUPPORTED, "T * (query heads per KV head) = %ld rows: at most %ld",
                   static_cast<long>(T) * map->group[n], kMaxGridY * per_wg);
   }
-  return MLKV_OK;
-}
-
-// MLKV_CHECK=1: every ctx_lens[b] in [0, capacity - T] (synchronizes).
-mlkv_status check_prefill_lengths_if_requested(const int32_t* ctx, int batch, int T, int S,
-                                               hipStream_t stream) {
-  const char* env = std::getenv("MLKV_CHECK");
-  if (!env || std::strcmp(env, "1") != 0) return MLKV_OK;
-  std::vector<int32_t> host(batch);
-  if (hipStreamSynchronize(stream) != hipSuccess ||
-      hipMemcpy(host.data(), ctx, sizeof(int32_t) * batch, hipMemcpyDeviceToHost) != hipSuccess)
-    return fail(MLKV_ERR_HIP, "MLKV_CHECK: could not read lengths back");
-  for (int b = 0; b < batch; ++b)
-    if (host[b] < 0 || static_cast<long>(host[b]) + T > S)
-      return fail(MLKV_ERR_CAPACITY, "MLKV_CHECK: sequence %d has %d cached + %d new tokens, "
-                  "capacity %d", b, host[b], T, S);
   return MLKV_OK;
 }
 
