@@ -365,6 +365,172 @@ mlkv_status mlkv_prefill_step(const void* q_all, const void* k_new_all, const vo
                               mlkv_out_dtype out_dtype, hipStream_t stream);
 
 /* ----------------------------------------------------------------------- */
+/* A cache held in 4 bits                                                    */
+/* ----------------------------------------------------------------------- */
+
+/*
+ * The cache of Section 2.4 in 4 bits a value: 3.76 times as many tokens in the
+ * same memory, on top of what sharing the heads saves (Section 3).  A token's
+ * key and value rows are held in blocks of 32 channels; a block's values are
+ * 2^e times one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign.  e is the least for
+ * which the block's largest magnitude is below 7 * 2^e, in [-124, 125]; each
+ * value is rounded to the nearest, ties to the even code.  Every value held is
+ * a bf16 number, and a row read back and stored again is held as before.  A
+ * block with a value that is not finite is held as NaN throughout.
+ *
+ * Caller-owned device memory of mlkv_qcache_bytes bytes, 16-byte aligned;
+ * capacity a multiple of 32, head_dim D 64 or 128.  One record of 34 D bytes
+ * for each 32 tokens, the record of tokens 32 n .. 32 n + 31 of (kv, b) at
+ * data + ((kv*batch + b)*(capacity/32) + n) * 34 D.  In a record, with K = D/32,
+ * token u = t & 31, channel d:
+ *   key code     nibble d & 1 (0: low) of byte (i >> 2)*1024 + l*16 + (i & 3)*4
+ *                + ((d & 7) >> 1), i = ((u >> 2) & 1)*K + (d >> 5),
+ *                l = ((d >> 3) & 3)*16 + ((u >> 3) << 2) + (u & 3)
+ *   value code   nibble u & 1 of byte 16 D + (j >> 2)*1024 + l*16 + (j & 3)*4
+ *                + ((u & 7) >> 1), j = d >> 4, l = (u >> 3)*16 + (d & 15)
+ *   key e + 127  byte 32 D + (((u >> 3) << 2) + (u & 3))*2 K + ((u >> 2) & 1)*K
+ *                + (d >> 5)
+ *   value e + 127  byte 33 D + (u >> 3)*8 K + (d >> 5)*8 + (u & 7)
+ *   code: bits 0-2 the place in the list above, bit 3 the sign; an exponent
+ *   byte of 255 makes the block NaN
+ * (the order in which a wave's matrix operands take a tile: one load
+ * instruction reads 1 KB of codes in one piece).
+ */
+typedef struct {
+  void* data;
+  int n_kv;
+  int batch;
+  int capacity;
+  int head_dim;
+} mlkv_qcache;
+
+/* n_kv * batch * capacity/32 * 34 * head_dim.  0 for invalid arguments. */
+size_t mlkv_qcache_bytes(const mlkv_map* map, int batch, int capacity, int head_dim);
+
+/* mlkv_cache_append_rows for the 4-bit cache: the T new rows (a decode step's
+ * newest token: T = 1) of the KV heads `layer` owns at slots ctx_lens[b] + t.
+ * Same arguments and errors; slots outside [0, capacity) are skipped, and
+ * nothing but the rows' slots changes. */
+mlkv_status mlkv_qcache_append_rows(int layer, const mlkv_map* map, const mlkv_qcache* cache,
+                                    const void* k_new, const void* v_new, int T,
+                                    int new_row_stride, const int32_t* ctx_lens,
+                                    hipStream_t stream);
+
+/* T rows of every sequence into, or out of, KV heads [kv_begin, kv_begin +
+ * kv_count): row t of sequence b is slot starts[b] + t.
+ *   starts: device int32 [batch], or NULL for 0.
+ *   T:      0 <= T <= capacity (else MLKV_ERR_CAPACITY).
+ *   k_rows, v_rows: device bf16 [kv_count][batch][T][head_dim], 16-byte aligned.
+ * Writing skips slots outside [0, capacity); reading returns zeros for them,
+ * and for other slots the values held (of a slot never stored: anything).
+ * With starts NULL and T = capacity: the whole cache, as
+ * mlkv_cache_write_rows / mlkv_cache_read_rows.  Errors as theirs. */
+mlkv_status mlkv_qcache_write_rows(const mlkv_qcache* cache, int kv_begin, int kv_count,
+                                   const int32_t* starts, int T, const void* k_rows,
+                                   const void* v_rows, hipStream_t stream);
+mlkv_status mlkv_qcache_read_rows(const mlkv_qcache* cache, int kv_begin, int kv_count,
+                                  const int32_t* starts, int T, void* k_rows, void* v_rows,
+                                  hipStream_t stream);
+
+/* ----------------------------------------------------------------------- */
+/* Attention over the 4-bit cache, and within a window                       */
+/* ----------------------------------------------------------------------- */
+
+/*
+ * mlkv_decode_attention of one layer within a window: with L = L_b, positions
+ * p < L with p < sinks or p >= L - window are attended (the newest `window`
+ * tokens, the newest one included, and the first `sinks`); the others are not
+ * read.
+ *   window: 0 for no limit (every position), else at least 1.
+ *   sinks:  at least 0.  Either may exceed the capacity.
+ * What is not attended has no influence, whatever it holds.  L_b = 0 gives
+ * zeros.  Any number of query heads per KV head.
+ * mlkv_qcache_decode_attention reads the 4-bit cache: keys and values are
+ * exactly those held.
+ *   max_len_hint: as mlkv_decode_attention (lengths above it are truncated).
+ *   workspace: device memory of at least mlkv_workspace_bytes_window(...)
+ *        bytes, 16-byte aligned, initialised once by mlkv_workspace_init; it
+ *        may be the same memory as that of the other decode calls if it is
+ *        large enough for both.  Calls that share one must be ordered.
+ * Results are bitwise reproducible.  Errors as mlkv_decode_attention, without
+ * its limits of group size and batch; MLKV_ERR_INVALID_ARG for a negative
+ * window or sinks; MLKV_ERR_UNSUPPORTED above about 16 million (sequence, KV
+ * head) units.
+ */
+mlkv_status mlkv_qcache_decode_attention(int layer, const void* q, const mlkv_qcache* cache,
+                                         const mlkv_map* map, const int32_t* seq_lens, int window,
+                                         int sinks, void* out, mlkv_out_dtype out_dtype,
+                                         int max_len_hint, void* workspace, size_t workspace_bytes,
+                                         hipStream_t stream);
+mlkv_status mlkv_decode_attention_window(int layer, const void* q, const mlkv_cache* cache,
+                                         const mlkv_map* map, const int32_t* seq_lens, int window,
+                                         int sinks, void* out, mlkv_out_dtype out_dtype,
+                                         int max_len_hint, void* workspace, size_t workspace_bytes,
+                                         hipStream_t stream);
+
+/* Workspace of those two for any layer, window, sinks and max_len_hint, on the
+ * current device.  0 for invalid arguments, and 0 when no call needs any. */
+size_t mlkv_workspace_bytes_window(const mlkv_map* map, int batch, int capacity, int head_dim);
+
+/* mlkv_prefill_attention within a window: token t of sequence b stands at
+ * position n = ctx_lens[b] + t and attends the positions p <= n with p < sinks
+ * or p > n - window (window and sinks as above; window 0: no limit).  Other
+ * arguments, limits and errors as mlkv_prefill_attention. */
+mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_cache* cache,
+                                          const mlkv_map* map, const int32_t* ctx_lens, int T,
+                                          int window, int sinks, void* out,
+                                          mlkv_out_dtype out_dtype, hipStream_t stream);
+
+/* ----------------------------------------------------------------------- */
+/* Norm and rotation of queries and keys, with the append                    */
+/* ----------------------------------------------------------------------- */
+
+/* What happens to a head vector x on its way: with a weight w (device bf16
+ * [head_dim], 16-byte aligned; NULL: no norm)
+ *   y_d = x_d * w_d / sqrt(mean_d x_d^2 + eps)
+ * and then, at position n, the channel pairs (j, j + rotary_dims/2), j <
+ * rotary_dims/2, turned by n * rotary_base^(-2j/rotary_dims) radians (as
+ * mlkv_decode_step_rope).  rotary_dims: a multiple of 16 in [0, head_dim]; 0:
+ * no rotation.  In fp32, the angle's turns in double, rounded once to bf16. */
+typedef struct {
+  const void* q_weight;
+  const void* k_weight;
+  double eps;
+  int rotary_dims;
+  double rotary_base;
+} mlkv_norm_rope;
+
+/*
+ * Between the projections and the attention of `layer`, in one launch: the
+ * queries of T new tokens normed and rotated into q_out, and, where the layer
+ * owns KV heads, the new keys normed and rotated and the new values as they
+ * are into their slots (mlkv_cache_append_rows / mlkv_qcache_append_rows of the
+ * same rows).  Token t of sequence b stands at position ctx_lens[b] + t.
+ *   q:     device bf16, row (b, t) at q + (b*T + t)*q_row_stride elements,
+ *          [h][head_dim]; q_row_stride a multiple of 8 and >= h*head_dim.
+ *   k_new, v_new: row (b, t) at + (b*T + t)*new_row_stride elements, the owned
+ *          heads back to back; new_row_stride a multiple of 8 and >=
+ *          owned*head_dim.  Not looked at where the layer owns no head.
+ *          (q, k_new and v_new may be columns of one projection's rows.)
+ *   T:     0 <= T <= capacity (else MLKV_ERR_CAPACITY); T = 0 does nothing.
+ *   q_out: device bf16 [batch][T][h][head_dim]; may be q itself when
+ *          q_row_stride is h*head_dim, and must not overlap anything else.
+ * Pointers 16-byte aligned.  The 4-bit form holds the bf16-rounded key.
+ * Errors: MLKV_ERR_INVALID_ARG, MLKV_ERR_ALIGNMENT, MLKV_ERR_CAPACITY,
+ * MLKV_ERR_UNSUPPORTED (rotary_dims, head_dim), MLKV_ERR_HIP.
+ */
+mlkv_status mlkv_norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* cache,
+                                  const void* q, int q_row_stride, const void* k_new,
+                                  const void* v_new, int new_row_stride, int T,
+                                  const int32_t* ctx_lens, const mlkv_norm_rope* norm_rope,
+                                  void* q_out, hipStream_t stream);
+mlkv_status mlkv_qcache_norm_rope_append(int layer, const mlkv_map* map, const mlkv_qcache* cache,
+                                         const void* q, int q_row_stride, const void* k_new,
+                                         const void* v_new, int new_row_stride, int T,
+                                         const int32_t* ctx_lens, const mlkv_norm_rope* norm_rope,
+                                         void* q_out, hipStream_t stream);
+
+/* ----------------------------------------------------------------------- */
 /* Model-level decode step: GPT-NeoX layers around the MLKV attention        */
 /* ----------------------------------------------------------------------- */
 

@@ -44,6 +44,10 @@ EXPORTS = [
     "mlkv_model_create", "mlkv_model_destroy", "mlkv_model_workspace_bytes",
     "mlkv_model_fused_path",
     "mlkv_model_decode_step",
+    "mlkv_qcache_bytes", "mlkv_qcache_append_rows", "mlkv_qcache_write_rows",
+    "mlkv_qcache_read_rows", "mlkv_qcache_decode_attention", "mlkv_decode_attention_window",
+    "mlkv_workspace_bytes_window", "mlkv_prefill_attention_window", "mlkv_norm_rope_append",
+    "mlkv_qcache_norm_rope_append",
 ]
 
 
@@ -58,6 +62,17 @@ class MLKVError(RuntimeError):
 class _Cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_kv", ctypes.c_int),
                 ("batch", ctypes.c_int), ("capacity", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class _QCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_kv", ctypes.c_int), ("batch", ctypes.c_int),
+                ("capacity", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+class _NormRope(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_double), ("rotary_dims", ctypes.c_int),
+                ("rotary_base", ctypes.c_double)]
 
 
 _lib = None
@@ -104,6 +119,16 @@ def lib():
             "mlkv_model_workspace_bytes": ([P, I, I], Z),
             "mlkv_model_fused_path": ([P, I], I),
             "mlkv_model_decode_step": ([P, P, P, P, I, P, Z, P], S),
+            "mlkv_qcache_bytes": ([P, I, I, I], Z),
+            "mlkv_qcache_append_rows": ([I, P, P, P, P, I, I, P, P], S),
+            "mlkv_qcache_write_rows": ([P, I, I, P, I, P, P, P], S),
+            "mlkv_qcache_read_rows": ([P, I, I, P, I, P, P, P], S),
+            "mlkv_qcache_decode_attention": ([I, P, P, P, P, I, I, P, I, I, P, Z, P], S),
+            "mlkv_decode_attention_window": ([I, P, P, P, P, I, I, P, I, I, P, Z, P], S),
+            "mlkv_workspace_bytes_window": ([P, I, I, I], Z),
+            "mlkv_prefill_attention_window": ([I, P, P, P, P, I, I, I, P, I, P], S),
+            "mlkv_norm_rope_append": ([I, P, P, P, I, P, P, I, I, P, P, P, P], S),
+            "mlkv_qcache_norm_rope_append": ([I, P, P, P, I, P, P, I, I, P, P, P, P], S),
             "mlkv_plan": ([P, I, I, I, I, I, ctypes.POINTER(I), ctypes.POINTER(I)], S),
             "mlkv_plan_merge_kernel": ([P, I, I, I, I, I], I),
             "mlkv_workspace_init": ([P, Z, P], S),
@@ -421,6 +446,220 @@ def prefill_step(q_all: torch.Tensor, k_new_all: torch.Tensor, v_new_all: torch.
                                    map_.handle, _dev_ptr(ctx_lens, torch.int32, "ctx_lens"),
                                    q_all.shape[2], _dev_ptr(out_all, out_all.dtype, "out_all"),
                                    out_dt, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Long contexts: a cache in 4 bits, attention within a window, norm and rotation
+# ---------------------------------------------------------------------------
+
+def _out_dtype(out: torch.Tensor) -> int:
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be float32 or bfloat16")
+    return OUT_BF16 if out.dtype == torch.bfloat16 else OUT_F32
+
+
+def _shaped(t: torch.Tensor, shape, name: str, dtype=torch.bfloat16) -> int:
+    """Device pointer of a contiguous tensor of exactly this shape."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev_ptr(t, dtype, name)
+
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """Elements between the [heads][D] rows of a bf16 device tensor
+    [B][T][heads][D] whose rows lie at one distance (T rows to a sequence)."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 4:
+        raise ValueError(f"{name} must be a bfloat16 device tensor [B][T][heads][D]")
+    B, T, heads, D = t.shape
+    sb, st, sh, sd = t.stride()
+    row = st if T > 1 else sb if B > 1 else heads * D
+    if (D > 1 and sd != 1) or (heads > 1 and sh != D) or (B > 1 and sb != T * row):
+        raise ValueError(f"{name}: rows must be contiguous and evenly spaced, strides {t.stride()}")
+    return row
+
+
+def _on_device(device: torch.device, *tensors):
+    """The tensors' device must be the current one: kernels are launched there."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {t.device} and {device}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {device}, current device {torch.cuda.current_device()}")
+
+
+def _ws_args(ws):
+    return (None, 0) if ws is None else (_dev_ptr(ws, ws.dtype, "ws"),
+                                         ws.numel() * ws.element_size())
+
+
+class QCache:
+    """The KV cache in 4 bits (mlkv_qcache): a uint8 tensor [n_kv][B][S/32][34 D]
+    in device memory, in the layout documented in mlkv.h.  write_rows and
+    read_rows convert from and to plain bf16 token rows."""
+
+    def __init__(self, data: torch.Tensor):
+        n_kv, B, tiles, record = data.shape
+        self.data = data
+        self.n_kv, self.batch, self.capacity = n_kv, B, tiles * V_BLOCK
+        self.head_dim = record // 34
+        if record not in (34 * 64, 34 * 128):
+            raise ValueError("data must be [n_kv][B][S/32][34 D] with D 64 or 128")
+        self._c = _QCache(_dev_ptr(data, torch.uint8, "data"), n_kv, B, self.capacity,
+                          self.head_dim)
+
+    @classmethod
+    def empty(cls, n_kv: int, batch: int, capacity: int, head_dim: int, device="cuda") -> "QCache":
+        if capacity % V_BLOCK:
+            raise ValueError("capacity must be a multiple of 32")
+        return cls(torch.empty((n_kv, batch, capacity // V_BLOCK, 34 * head_dim),
+                               dtype=torch.uint8, device=device))
+
+    @property
+    def struct(self):
+        return ctypes.byref(self._c)
+
+    def _starts(self, starts):
+        if starts is None:
+            return None
+        return _shaped(starts, (self.batch,), "starts", torch.int32)
+
+    def write_rows(self, k_rows: torch.Tensor, v_rows: torch.Tensor, kv_begin: int = 0,
+                   starts: torch.Tensor | None = None, stream=None):
+        """mlkv_qcache_write_rows: bf16 rows [n][B][T][D] into KV heads kv_begin ..
+        kv_begin + n - 1, row t of sequence b at slot starts[b] + t (default: t)."""
+        _on_device(self.data.device, k_rows, v_rows, starts)
+        n, _, T, _ = k_rows.shape
+        shape = (n, self.batch, T, self.head_dim)
+        _check(lib().mlkv_qcache_write_rows(self.struct, kv_begin, n, self._starts(starts), T,
+                                            _shaped(k_rows, shape, "k_rows"),
+                                            _shaped(v_rows, shape, "v_rows"), _stream(stream)))
+
+    def read_rows(self, kv_begin: int = 0, kv_count: int | None = None,
+                  starts: torch.Tensor | None = None, T: int | None = None, stream=None):
+        """mlkv_qcache_read_rows: the values held, as rows (k, v), each bf16
+        [kv_count][B][T][D]; T defaults to the capacity."""
+        _on_device(self.data.device, starts)
+        n = self.n_kv - kv_begin if kv_count is None else kv_count
+        T = self.capacity if T is None else T
+        shape = (n, self.batch, T, self.head_dim)
+        k = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
+        v = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
+        if isinstance(stream, torch.cuda.Stream):  # the rows are written there
+            k.record_stream(stream)
+            v.record_stream(stream)
+        _check(lib().mlkv_qcache_read_rows(self.struct, kv_begin, n, self._starts(starts), T,
+                                           k.data_ptr(), v.data_ptr(), _stream(stream)))
+        return k, v
+
+
+def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor,
+                       v_new: torch.Tensor, ctx_lens: torch.Tensor, stream=None):
+    """mlkv_qcache_append_rows: k_new/v_new [B][T][owned][D] (rows may be columns
+    of a wider tensor's), stored at slots ctx_lens[b] + t."""
+    _on_device(cache.data.device, k_new, v_new, ctx_lens)
+    stride = _new_rows(layer, map_, cache, k_new, v_new)
+    _check(lib().mlkv_qcache_append_rows(layer, map_.handle, cache.struct, k_new.data_ptr(),
+                                         v_new.data_ptr(), k_new.shape[1], stride,
+                                         _shaped(ctx_lens, (cache.batch,), "ctx_lens", torch.int32),
+                                         _stream(stream)))
+
+
+def _new_rows(layer: int, map_: Map, cache, k_new: torch.Tensor, v_new: torch.Tensor) -> int:
+    """The row stride of a layer's new keys and values."""
+    shape = (cache.batch, k_new.shape[1], map_.layer_owned(layer)[1], cache.head_dim)
+    stride = _row_stride(k_new, "k_new")
+    if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape:
+        raise ValueError(f"k_new and v_new must be {shape}")
+    if _row_stride(v_new, "v_new") != stride:
+        raise ValueError("k_new and v_new must have rows at the same distance")
+    return stride
+
+
+def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda",
+                     stream=None) -> torch.Tensor:
+    """Allocate and initialise a workspace of mlkv_workspace_bytes_window bytes."""
+    n = lib().mlkv_workspace_bytes_window(map_.handle, batch, capacity, head_dim)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    _check(lib().mlkv_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)))
+    return ws
+
+
+def _window_attention(f, layer, q, cache, device, map_, seq_lens, out, window, sinks, max_len_hint,
+                      ws, stream):
+    _on_device(device, q, seq_lens, out, ws)
+    shape = (cache.batch, map_.h, cache.head_dim)
+    _check(f(layer, _shaped(q, shape, "q"), cache.struct, map_.handle,
+             _shaped(seq_lens, (cache.batch,), "seq_lens", torch.int32), window, sinks,
+             _shaped(out, shape, "out", out.dtype), _out_dtype(out), max_len_hint, *_ws_args(ws),
+             _stream(stream)))
+
+
+def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Map,
+                            seq_lens: torch.Tensor, out: torch.Tensor, window: int = 0,
+                            sinks: int = 0, max_len_hint: int = 0,
+                            ws: torch.Tensor | None = None, stream=None):
+    """mlkv_qcache_decode_attention: q [B][h][D] bf16 over the 4-bit cache ->
+    out [B][h][D] (fp32 or bf16); ws from window_workspace."""
+    _window_attention(lib().mlkv_qcache_decode_attention, layer, q, cache, cache.data.device, map_,
+                      seq_lens, out, window, sinks, max_len_hint, ws, stream)
+
+
+def decode_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Map,
+                            seq_lens: torch.Tensor, out: torch.Tensor, window: int,
+                            sinks: int = 0, max_len_hint: int = 0,
+                            ws: torch.Tensor | None = None, stream=None):
+    """mlkv_decode_attention_window: the newest `window` positions and the
+    first `sinks`; ws from window_workspace."""
+    _window_attention(lib().mlkv_decode_attention_window, layer, q, cache, cache.k.device, map_,
+                      seq_lens, out, window, sinks, max_len_hint, ws, stream)
+
+
+def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Map,
+                             ctx_lens: torch.Tensor, out: torch.Tensor, window: int,
+                             sinks: int = 0, stream=None):
+    """mlkv_prefill_attention_window: q [B][T][h][D] bf16 -> out [B][T][h][D]
+    (fp32 or bf16); token t of sequence b stands at position ctx_lens[b] + t."""
+    _on_device(cache.k.device, q, ctx_lens, out)
+    shape = (cache.batch, q.shape[1], map_.h, cache.head_dim)
+    _check(lib().mlkv_prefill_attention_window(
+        layer, _shaped(q, shape, "q"), cache.struct, map_.handle,
+        _shaped(ctx_lens, (cache.batch,), "ctx_lens", torch.int32), shape[1], window, sinks,
+        _shaped(out, shape, "out", out.dtype), _out_dtype(out), _stream(stream)))
+
+
+def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch.Tensor | None,
+                     v_new: torch.Tensor | None, ctx_lens: torch.Tensor, q_out: torch.Tensor,
+                     q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None,
+                     eps: float = 1e-6, rotary_dims: int = 0, rotary_base: float = 10000.0,
+                     stream=None):
+    """mlkv_norm_rope_append (cache a Cache) or mlkv_qcache_norm_rope_append (a
+    QCache): queries q [B][T][h][D] normed per head (weights q_norm [D]; None:
+    not) and rotated into q_out [B][T][h][D], and the layer's new keys (k_norm)
+    and values [B][T][owned][D] stored at slots ctx_lens[b] + t (k_new and v_new
+    None where the layer owns no head).  q, k_new and v_new may be columns of
+    one projection's rows."""
+    four_bits = isinstance(cache, QCache)
+    device = cache.data.device if four_bits else cache.k.device
+    _on_device(device, q, k_new, v_new, ctx_lens, q_out, q_norm, k_norm)
+    B, T, h, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
+    if (B, h, D) != (cache.batch, map_.h, cache.head_dim):
+        raise ValueError(f"q must be [{cache.batch}][T][{map_.h}][{cache.head_dim}]")
+    kp = vp = None
+    stride = 0
+    if map_.layer_owned(layer)[1]:
+        if k_new is None or v_new is None:
+            raise ValueError(f"layer {layer} owns KV heads: k_new and v_new are needed")
+        stride = _new_rows(layer, map_, cache, k_new, v_new)
+        if k_new.shape[1] != T:
+            raise ValueError(f"q has {T} tokens, k_new {k_new.shape[1]}")
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    weights = [None if w is None else _shaped(w, (D,), name)
+               for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
+    nr = _NormRope(*weights, float(eps), rotary_dims, float(rotary_base))
+    f = lib().mlkv_qcache_norm_rope_append if four_bits else lib().mlkv_norm_rope_append
+    _check(f(layer, map_.handle, cache.struct, q.data_ptr(), _row_stride(q, "q"), kp, vp, stride, T,
+             _shaped(ctx_lens, (B,), "ctx_lens", torch.int32), ctypes.byref(nr),
+             _shaped(q_out, (B, T, h, D), "q_out"), _stream(stream)))
 
 
 # ---------------------------------------------------------------- model ---

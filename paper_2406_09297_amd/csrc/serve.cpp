@@ -1,0 +1,479 @@
+// C ABI of the long-context serving operators: the 4-bit cache, attention over
+// it or within a window, norm and rotation before the append.  Every argument
+// error is reported before any HIP call.
+#include "mlkv.h"
+
+#include <cmath>
+
+#include "host.h"
+#include "serve.h"
+
+using namespace mlkv::host;
+
+namespace {
+
+mlkv_status check_qcache(const mlkv_qcache* c) {
+  if (!c) return fail(MLKV_ERR_INVALID_ARG, "cache is NULL");
+  if (!c->data) return fail(MLKV_ERR_INVALID_ARG, "cache data must be non-NULL");
+  if (!aligned16(c->data)) return fail(MLKV_ERR_ALIGNMENT, "cache data must be 16-byte aligned");
+  if (c->batch <= 0 || c->capacity <= 0 || c->n_kv <= 0)
+    return fail(MLKV_ERR_INVALID_ARG, "cache n_kv, batch and capacity must be positive");
+  if (c->capacity % kTileTokens != 0)
+    return fail(MLKV_ERR_CAPACITY, "cache capacity %d is not a multiple of 32", c->capacity);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(MLKV_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", c->head_dim);
+  const double elems = 2.0 * c->n_kv * c->batch * static_cast<double>(c->capacity) * c->head_dim;
+  if (elems > 9.0e18) return fail(MLKV_ERR_CAPACITY, "cache too large");
+  return MLKV_OK;
+}
+
+mlkv_status check_qcache(const mlkv_qcache* c, const mlkv_map* map) {
+  const mlkv_status s = check_qcache(c);
+  if (s != MLKV_OK) return s;
+  if (c->n_kv != map->n_kv)
+    return fail(MLKV_ERR_INVALID_ARG, "cache has %d KV heads, map has %d", c->n_kv, map->n_kv);
+  return MLKV_OK;
+}
+
+mlkv_status check_layer(const mlkv_map* map, int layer) {
+  const mlkv_status s = check_map(map);
+  if (s != MLKV_OK) return s;
+  if (layer < 0 || layer >= map->l)
+    return fail(MLKV_ERR_INVALID_ARG, "layer %d out of range", layer);
+  return MLKV_OK;
+}
+
+mlkv_status check_tokens(int T, int capacity) {
+  if (T < 0 || T > capacity)
+    return fail(MLKV_ERR_CAPACITY, "T = %d new tokens: must be in [0, capacity %d]", T, capacity);
+  return MLKV_OK;
+}
+
+mlkv_status check_new_rows(const void* k_new, const void* v_new, int row_stride, int owned,
+                           int head_dim) {
+  if (!k_new || !v_new) return fail(MLKV_ERR_INVALID_ARG, "k_new and v_new must be non-NULL");
+  if (!aligned16(k_new) || !aligned16(v_new))
+    return fail(MLKV_ERR_ALIGNMENT, "k_new and v_new must be 16-byte aligned");
+  if (row_stride % 8 != 0 || row_stride < static_cast<long>(owned) * head_dim)
+    return fail(MLKV_ERR_INVALID_ARG, "new_row_stride %d must be a multiple of 8 and >= %ld",
+                row_stride, static_cast<long>(owned) * head_dim);
+  return MLKV_OK;
+}
+
+mlkv_status check_window(int window, int sinks) {
+  if (window < 0 || sinks < 0)
+    return fail(MLKV_ERR_INVALID_ARG, "window %d and sinks %d must not be negative", window, sinks);
+  return MLKV_OK;
+}
+
+// Tiles that T rows from any slot on may touch.
+int touched_tiles(int T, bool from_zero) {
+  const long first = from_zero ? 0 : kTileTokens - 1;
+  return static_cast<int>((T + first + kTileTokens - 1) / kTileTokens);
+}
+
+mlkv::StoreParams store_params(const mlkv_qcache* q4, const mlkv_cache* bf16, int T, int kv_begin,
+                               int kv_count, const int32_t* starts) {
+  mlkv::StoreParams p{};
+  if (q4) {
+    p.q4 = static_cast<uint8_t*>(q4->data);
+    p.B = q4->batch;
+    p.S = q4->capacity;
+  } else {
+    p.k = static_cast<uint16_t*>(bf16->k);
+    p.v = static_cast<uint16_t*>(bf16->v);
+    p.B = bf16->batch;
+    p.S = bf16->capacity;
+  }
+  p.T = T;
+  p.kv_begin = kv_begin;
+  p.kv_count = kv_count;
+  p.starts = starts;
+  p.tiles = touched_tiles(T, !starts);
+  p.store_items = static_cast<long>(kv_count) * p.B * p.tiles;
+  return p;
+}
+
+mlkv_status launch_store_checked(const mlkv::StoreParams& p, int head_dim, bool norm,
+                                 hipStream_t stream) {
+  const hipError_t err = mlkv::launch_store(p, head_dim, norm, stream);
+  if (err != hipSuccess) return fail(MLKV_ERR_HIP, "append launch: %s", hipGetErrorString(err));
+  return ok();
+}
+
+// Rows of heads [kv_begin, kv_begin + kv_count) of a 4-bit cache, in or out.
+mlkv_status check_rows(const mlkv_qcache* cache, int kv_begin, int kv_count, const int32_t* starts,
+                       int T) {
+  mlkv_status s;
+  if ((s = check_qcache(cache)) != MLKV_OK) return s;
+  if (kv_begin < 0 || kv_count < 0 || kv_begin + static_cast<long>(kv_count) > cache->n_kv)
+    return fail(MLKV_ERR_INVALID_ARG, "KV heads [%d, %d + %d) outside [0, %d)", kv_begin, kv_begin,
+                kv_count, cache->n_kv);
+  if ((s = check_tokens(T, cache->capacity)) != MLKV_OK) return s;
+  if (!aligned4(starts)) return fail(MLKV_ERR_ALIGNMENT, "starts must be 4-byte aligned");
+  return MLKV_OK;
+}
+
+mlkv_status check_row_buffers(const void* k_rows, const void* v_rows) {
+  if (!k_rows || !v_rows) return fail(MLKV_ERR_INVALID_ARG, "k_rows and v_rows must be non-NULL");
+  if (!aligned16(k_rows) || !aligned16(v_rows))
+    return fail(MLKV_ERR_ALIGNMENT, "k_rows and v_rows must be 16-byte aligned");
+  return MLKV_OK;
+}
+
+// How a layer's (sequence, KV head) units are cut (span.hip): `chunks` parts of
+// the G query rows, runs of run_tiles tiles, at most `runs` of a unit.
+struct SpanPlan {
+  int chunks, chunk_rows, runs, run_tiles;
+  long units;
+  size_t ml, need;  // offset of the (max, denominator) pairs, bytes in all; 0 without split runs
+};
+constexpr int kSpanMinTiles = 8;     // least tiles of a run
+constexpr long kSpanGroupsPerCu = 4;  // workgroups a compute unit is given by splitting
+
+SpanPlan span_plan(const mlkv_map* map, int layer, int batch, int head_dim, int max_len, int window,
+                   int sinks) {
+  SpanPlan pl{};
+  const int G = map->group[layer];
+  const int blocks = (G + 15) / 16;
+  pl.units = static_cast<long>(batch) * map->kv_count[layer];
+  pl.chunks = (blocks + mlkv::kSpanMaxBlocks - 1) / mlkv::kSpanMaxBlocks;
+  pl.chunk_rows = (G + pl.chunks - 1) / pl.chunks;
+  int tiles = tiles_of(max_len < 1 ? 1 : max_len);
+  if (window > 0) {  // both ends of the window and the first tokens' end inside a tile
+    const long most = tiles_of(window) + 1L + (sinks + static_cast<long>(kTileTokens) - 1) / kTileTokens;
+    tiles = static_cast<int>(tiles < most ? tiles : most);
+  }
+  const long groups = pl.units * pl.chunks;
+  long runs = kSpanGroupsPerCu * compute_units_or_fallback() / groups;
+  const long longest = tiles / kSpanMinTiles;
+  runs = runs < longest ? runs : longest;
+  pl.runs = static_cast<int>(runs < 1 ? 1 : runs);
+  pl.run_tiles = (tiles + pl.runs - 1) / pl.runs;
+  if (pl.runs > 1) {
+    const size_t part_rows = static_cast<size_t>(groups) * pl.runs * pl.chunk_rows;
+    pl.ml = kCounterSlots * sizeof(int32_t) + align_up(part_rows * head_dim * sizeof(float), 256);
+    pl.need = pl.ml + part_rows * 2 * sizeof(float);
+  }
+  return pl;
+}
+
+mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, const mlkv_qcache* q4,
+                           const mlkv_map* map, const int32_t* seq_lens, int window, int sinks,
+                           void* out, mlkv_out_dtype out_dtype, int max_len_hint, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream) {
+  const int B = q4 ? q4->batch : bf16->batch, S = q4 ? q4->capacity : bf16->capacity;
+  const int D = q4 ? q4->head_dim : bf16->head_dim;
+  if (!q || !seq_lens || !out)
+    return fail(MLKV_ERR_INVALID_ARG, "q, seq_lens, out must be non-NULL");
+  if (!aligned16(q) || !aligned16(out))
+    return fail(MLKV_ERR_ALIGNMENT, "q and out must be 16-byte aligned");
+  if (!aligned4(seq_lens)) return fail(MLKV_ERR_ALIGNMENT, "seq_lens must be 4-byte aligned");
+  if (out_dtype != MLKV_OUT_F32 && out_dtype != MLKV_OUT_BF16)
+    return fail(MLKV_ERR_INVALID_ARG, "bad out_dtype");
+  mlkv_status s;
+  if ((s = check_window(window, sinks)) != MLKV_OK) return s;
+  if (max_len_hint > S)
+    return fail(MLKV_ERR_CAPACITY, "max_len_hint %d above capacity %d", max_len_hint, S);
+  const int max_len = max_len_hint <= 0 ? S : max_len_hint;
+  window = window < S ? window : S;  // larger ones say the same
+  sinks = sinks < S ? sinks : S;
+  const SpanPlan pl = span_plan(map, layer, B, D, max_len, window, sinks);
+  // A grid has fewer than 2^32 threads.
+  if (static_cast<double>(pl.units) * pl.runs * pl.chunks >= (1L << 24) - 8.0 * pl.chunks)
+    return fail(MLKV_ERR_UNSUPPORTED, "%ld (sequence, KV head) units: more than one launch takes",
+                pl.units);
+  if (pl.need > 0 && (!workspace || workspace_bytes < pl.need))
+    return fail(MLKV_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", pl.need,
+                workspace ? workspace_bytes : 0);
+  if (pl.need > 0 && !aligned16(workspace))
+    return fail(MLKV_ERR_ALIGNMENT, "workspace not 16-byte aligned");
+  if ((s = check_lengths_if_requested(seq_lens, B, 0, max_len, stream)) != MLKV_OK) return s;
+  mlkv::SpanParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  if (q4) {
+    p.q4 = static_cast<const uint8_t*>(q4->data);
+  } else {
+    p.k = static_cast<const uint16_t*>(bf16->k);
+    p.v = static_cast<const uint16_t*>(bf16->v);
+  }
+  p.lens = seq_lens;
+  p.out = out;
+  if (pl.need > 0) {
+    char* base = static_cast<char*>(workspace);
+    p.counters = reinterpret_cast<int*>(base);
+    p.part_acc = reinterpret_cast<float*>(base + kCounterSlots * sizeof(int32_t));
+    p.part_ml = reinterpret_cast<float*>(base + pl.ml);
+  }
+  p.B = B;
+  p.h = map->h;
+  p.S = S;
+  p.kv_begin = map->kv_begin[layer];
+  p.n_groups = map->kv_count[layer];
+  p.G = map->group[layer];
+  p.chunks = pl.chunks;
+  p.chunk_rows = pl.chunk_rows;
+  p.runs = pl.runs;
+  p.run_tiles = pl.run_tiles;
+  p.items = static_cast<unsigned>(pl.units * pl.runs);
+  p.max_len = max_len;
+  p.window = window;
+  p.sinks = sinks;
+  p.out_bf16 = out_dtype == MLKV_OUT_BF16 ? 1 : 0;
+  p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(D)));
+  Profile& prof = g_profile;
+  const bool timed = prof.on && prof.used < static_cast<int>(prof.start.size());
+  const hipError_t err = mlkv::launch_span(p, D, stream, timed ? prof.start[prof.used] : nullptr,
+                                           timed ? prof.stop[prof.used] : nullptr);
+  if (err != hipSuccess) return fail(MLKV_ERR_HIP, "attention launch: %s", hipGetErrorString(err));
+  if (timed) ++prof.used;
+  return ok();
+}
+
+mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* bf16,
+                             const mlkv_qcache* q4, const void* q, int q_row_stride,
+                             const void* k_new, const void* v_new, int new_row_stride, int T,
+                             const int32_t* ctx_lens, const mlkv_norm_rope* nr, void* q_out,
+                             hipStream_t stream) {
+  const int B = q4 ? q4->batch : bf16->batch, S = q4 ? q4->capacity : bf16->capacity;
+  const int D = q4 ? q4->head_dim : bf16->head_dim, h = map->h, owned = map->own_count[layer];
+  mlkv_status s;
+  if ((s = check_tokens(T, S)) != MLKV_OK) return s;
+  if (!nr) return fail(MLKV_ERR_INVALID_ARG, "norm_rope is NULL");
+  if (nr->rotary_dims < 0 || nr->rotary_dims > D || nr->rotary_dims % 16 != 0)
+    return fail(MLKV_ERR_UNSUPPORTED, "rotary_dims %d: a multiple of 16 in [0, head_dim] required",
+                nr->rotary_dims);
+  if (nr->rotary_dims > 0 && (!(nr->rotary_base > 0.0) || !std::isfinite(nr->rotary_base)))
+    return fail(MLKV_ERR_INVALID_ARG, "rotary_base must be positive and finite");
+  if (!(nr->eps >= 0.0) || !std::isfinite(nr->eps))
+    return fail(MLKV_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (!aligned16(nr->q_weight) || !aligned16(nr->k_weight))
+    return fail(MLKV_ERR_ALIGNMENT, "norm weights must be 16-byte aligned");
+  if (T == 0) return ok();
+  if (!q || !q_out || !ctx_lens)
+    return fail(MLKV_ERR_INVALID_ARG, "q, q_out and ctx_lens must be non-NULL");
+  if (!aligned16(q) || !aligned16(q_out))
+    return fail(MLKV_ERR_ALIGNMENT, "q and q_out must be 16-byte aligned");
+  if (!aligned4(ctx_lens)) return fail(MLKV_ERR_ALIGNMENT, "ctx_lens must be 4-byte aligned");
+  if (q_row_stride % 8 != 0 || q_row_stride < static_cast<long>(h) * D)
+    return fail(MLKV_ERR_INVALID_ARG, "q_row_stride %d must be a multiple of 8 and >= %ld",
+                q_row_stride, static_cast<long>(h) * D);
+  if (owned > 0 && (s = check_new_rows(k_new, v_new, new_row_stride, owned, D)) != MLKV_OK) return s;
+  if ((s = check_prefill_lengths_if_requested(ctx_lens, B, T, S, stream)) != MLKV_OK) return s;
+  mlkv::StoreParams p =
+      store_params(q4, bf16, T, owned > 0 ? map->own_begin[layer] : 0, owned, ctx_lens);
+  p.k_src = static_cast<const uint16_t*>(k_new);
+  p.v_src = static_cast<const uint16_t*>(v_new);
+  p.s_head = D;
+  p.s_tok = new_row_stride;
+  p.s_seq = static_cast<size_t>(T) * new_row_stride;
+  p.q_w = static_cast<const uint16_t*>(nr->q_weight);
+  p.k_w = static_cast<const uint16_t*>(nr->k_weight);
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_out = static_cast<uint16_t*>(q_out);
+  p.q_stride = q_row_stride;
+  p.h = h;
+  // Eight tokens share the sines of a query workgroup.
+  p.q_tokens = T < 8 ? T : 8;
+  p.q_items = static_cast<long>(B) * ((T + p.q_tokens - 1) / p.q_tokens);
+  p.half = nr->rotary_dims / 2;
+  p.eps = static_cast<float>(nr->eps);
+  for (int j = 0; j < p.half; ++j)
+    p.turns[j] = std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims) * 0.15915494309189533577;
+  return launch_store_checked(p, D, true, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mlkv_qcache_bytes(const mlkv_map* map, int batch, int capacity, int head_dim) {
+  if (!map || batch <= 0 || capacity <= 0 || capacity % kTileTokens != 0 ||
+      (head_dim != 64 && head_dim != 128))
+    return 0;
+  return static_cast<size_t>(map->n_kv) * batch * (capacity / kTileTokens) *
+         mlkv::kQTileBytes(head_dim);
+}
+
+mlkv_status mlkv_qcache_append_rows(int layer, const mlkv_map* map, const mlkv_qcache* cache,
+                                    const void* k_new, const void* v_new, int T,
+                                    int new_row_stride, const int32_t* ctx_lens,
+                                    hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_qcache(cache, map)) != MLKV_OK) return s;
+  if ((s = check_tokens(T, cache->capacity)) != MLKV_OK) return s;
+  const int owned = map->own_count[layer];
+  if (owned == 0 || T == 0) return ok();
+  if ((s = check_new_rows(k_new, v_new, new_row_stride, owned, cache->head_dim)) != MLKV_OK)
+    return s;
+  if (!ctx_lens) return fail(MLKV_ERR_INVALID_ARG, "ctx_lens must be non-NULL");
+  if (!aligned4(ctx_lens)) return fail(MLKV_ERR_ALIGNMENT, "ctx_lens must be 4-byte aligned");
+  if ((s = check_prefill_lengths_if_requested(ctx_lens, cache->batch, T, cache->capacity,
+                                              stream)) != MLKV_OK)
+    return s;
+  mlkv::StoreParams p = store_params(cache, nullptr, T, map->own_begin[layer], owned, ctx_lens);
+  p.k_src = static_cast<const uint16_t*>(k_new);
+  p.v_src = static_cast<const uint16_t*>(v_new);
+  p.s_head = cache->head_dim;
+  p.s_tok = new_row_stride;
+  p.s_seq = static_cast<size_t>(T) * new_row_stride;
+  return launch_store_checked(p, cache->head_dim, false, stream);
+}
+
+mlkv_status mlkv_qcache_write_rows(const mlkv_qcache* cache, int kv_begin, int kv_count,
+                                   const int32_t* starts, int T, const void* k_rows,
+                                   const void* v_rows, hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_rows(cache, kv_begin, kv_count, starts, T)) != MLKV_OK) return s;
+  if (kv_count == 0 || T == 0) return ok();
+  if ((s = check_row_buffers(k_rows, v_rows)) != MLKV_OK) return s;
+  mlkv::StoreParams p = store_params(cache, nullptr, T, kv_begin, kv_count, starts);
+  p.k_src = static_cast<const uint16_t*>(k_rows);
+  p.v_src = static_cast<const uint16_t*>(v_rows);
+  p.s_tok = cache->head_dim;
+  p.s_seq = p.s_tok * T;
+  p.s_head = p.s_seq * cache->batch;
+  return launch_store_checked(p, cache->head_dim, false, stream);
+}
+
+mlkv_status mlkv_qcache_read_rows(const mlkv_qcache* cache, int kv_begin, int kv_count,
+                                  const int32_t* starts, int T, void* k_rows, void* v_rows,
+                                  hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_rows(cache, kv_begin, kv_count, starts, T)) != MLKV_OK) return s;
+  if (kv_count == 0 || T == 0) return ok();
+  if ((s = check_row_buffers(k_rows, v_rows)) != MLKV_OK) return s;
+  mlkv::ReadParams p{};
+  p.q4 = static_cast<const uint8_t*>(cache->data);
+  p.k_rows = static_cast<uint16_t*>(k_rows);
+  p.v_rows = static_cast<uint16_t*>(v_rows);
+  p.starts = starts;
+  p.B = cache->batch;
+  p.T = T;
+  p.S = cache->capacity;
+  p.kv_begin = kv_begin;
+  p.kv_count = kv_count;
+  p.tiles = touched_tiles(T, !starts);
+  p.items = static_cast<long>(kv_count) * p.B * p.tiles;
+  const hipError_t err = mlkv::launch_qcache_read(p, cache->head_dim, stream);
+  if (err != hipSuccess) return fail(MLKV_ERR_HIP, "cache rows launch: %s", hipGetErrorString(err));
+  return ok();
+}
+
+size_t mlkv_workspace_bytes_window(const mlkv_map* map, int batch, int capacity, int head_dim) {
+  if (!map || batch <= 0 || capacity <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  // The most runs are those without a window at the capacity.
+  size_t most = 0;
+  for (int n = 0; n < map->l; ++n) {
+    const size_t need = span_plan(map, n, batch, head_dim, capacity, 0, 0).need;
+    most = need > most ? need : most;
+  }
+  return most;
+}
+
+mlkv_status mlkv_qcache_decode_attention(int layer, const void* q, const mlkv_qcache* cache,
+                                         const mlkv_map* map, const int32_t* seq_lens, int window,
+                                         int sinks, void* out, mlkv_out_dtype out_dtype,
+                                         int max_len_hint, void* workspace, size_t workspace_bytes,
+                                         hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_qcache(cache, map)) != MLKV_OK) return s;
+  return span_attention(layer, q, nullptr, cache, map, seq_lens, window, sinks, out, out_dtype,
+                        max_len_hint, workspace, workspace_bytes, stream);
+}
+
+mlkv_status mlkv_decode_attention_window(int layer, const void* q, const mlkv_cache* cache,
+                                         const mlkv_map* map, const int32_t* seq_lens, int window,
+                                         int sinks, void* out, mlkv_out_dtype out_dtype,
+                                         int max_len_hint, void* workspace, size_t workspace_bytes,
+                                         hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_cache(cache, map)) != MLKV_OK) return s;
+  return span_attention(layer, q, cache, nullptr, map, seq_lens, window, sinks, out, out_dtype,
+                        max_len_hint, workspace, workspace_bytes, stream);
+}
+
+mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_cache* cache,
+                                          const mlkv_map* map, const int32_t* ctx_lens, int T,
+                                          int window, int sinks, void* out,
+                                          mlkv_out_dtype out_dtype, hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_cache(cache, map)) != MLKV_OK) return s;
+  if ((s = check_tokens(T, cache->capacity)) != MLKV_OK) return s;
+  if ((s = check_window(window, sinks)) != MLKV_OK) return s;
+  const int B = cache->batch, D = cache->head_dim, G = map->group[layer];
+  const long per_wg = mlkv::prefill_rows_per_workgroup(D);
+  if ((static_cast<long>(T) * G + per_wg - 1) / per_wg > kMaxGridY)
+    return fail(MLKV_ERR_UNSUPPORTED, "T * (query heads per KV head) = %ld rows: at most %ld",
+                static_cast<long>(T) * G, kMaxGridY * per_wg);
+  if (static_cast<long>(B) * map->kv_count[layer] >= mlkv::kMaxPrefillUnits)
+    return fail(MLKV_ERR_UNSUPPORTED, "%ld (sequence, KV head) units: at most %ld",
+                static_cast<long>(B) * map->kv_count[layer], mlkv::kMaxPrefillUnits - 1);
+  if (!q || !ctx_lens || !out)
+    return fail(MLKV_ERR_INVALID_ARG, "q, ctx_lens, out must be non-NULL");
+  if (!aligned16(q) || !aligned16(out))
+    return fail(MLKV_ERR_ALIGNMENT, "q and out must be 16-byte aligned");
+  if (!aligned4(ctx_lens)) return fail(MLKV_ERR_ALIGNMENT, "ctx_lens must be 4-byte aligned");
+  if (out_dtype != MLKV_OUT_F32 && out_dtype != MLKV_OUT_BF16)
+    return fail(MLKV_ERR_INVALID_ARG, "bad out_dtype");
+  if ((s = check_prefill_lengths_if_requested(ctx_lens, B, T, cache->capacity, stream)) != MLKV_OK)
+    return s;
+  if (T == 0) return ok();
+  mlkv::WindowPrefillParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(cache->k);
+  p.v = static_cast<const uint16_t*>(cache->v);
+  p.ctx = ctx_lens;
+  p.out = out;
+  p.B = B;
+  p.T = T;
+  p.h = map->h;
+  p.S = cache->capacity;
+  p.kv_begin = map->kv_begin[layer];
+  p.G = G;
+  p.n_groups = map->kv_count[layer];
+  p.layers = 1;
+  p.kv_per_layer = p.n_groups;
+  p.out_bf16 = out_dtype == MLKV_OUT_BF16 ? 1 : 0;
+  p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(D)));
+  p.window = window < p.S ? window : p.S;  // larger ones say the same
+  p.sinks = sinks < p.S ? sinks : p.S;
+  Profile& prof = g_profile;
+  const bool timed = prof.on && prof.used < static_cast<int>(prof.start.size());
+  const hipError_t err =
+      mlkv::launch_prefill_window(p, D, stream, timed ? prof.start[prof.used] : nullptr,
+                                  timed ? prof.stop[prof.used] : nullptr);
+  if (err != hipSuccess) return fail(MLKV_ERR_HIP, "prefill launch: %s", hipGetErrorString(err));
+  if (timed) ++prof.used;
+  return ok();
+}
+
+mlkv_status mlkv_norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* cache,
+                                  const void* q, int q_row_stride, const void* k_new,
+                                  const void* v_new, int new_row_stride, int T,
+                                  const int32_t* ctx_lens, const mlkv_norm_rope* norm_rope,
+                                  void* q_out, hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_cache(cache, map)) != MLKV_OK) return s;
+  return norm_rope_append(layer, map, cache, nullptr, q, q_row_stride, k_new, v_new,
+                          new_row_stride, T, ctx_lens, norm_rope, q_out, stream);
+}
+
+mlkv_status mlkv_qcache_norm_rope_append(int layer, const mlkv_map* map, const mlkv_qcache* cache,
+                                         const void* q, int q_row_stride, const void* k_new,
+                                         const void* v_new, int new_row_stride, int T,
+                                         const int32_t* ctx_lens, const mlkv_norm_rope* norm_rope,
+                                         void* q_out, hipStream_t stream) {
+  mlkv_status s;
+  if ((s = check_layer(map, layer)) != MLKV_OK) return s;
+  if ((s = check_qcache(cache, map)) != MLKV_OK) return s;
+  return norm_rope_append(layer, map, nullptr, cache, q, q_row_stride, k_new, v_new,
+                          new_row_stride, T, ctx_lens, norm_rope, q_out, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,212 @@
+"""Norm and rotation of queries and keys with the append, against the plain
+64-bit statement (tests/serve_ref.py), and the operators together as one
+layer of a serving program uses them."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import serve_ref  # noqa: E402
+import synth  # noqa: E402
+from gpu_util import say  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+mlkv = pytest.importorskip("paper_2406_09297_amd")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    mlkv.lib()
+    yield
+
+
+def _projected(seed, B, T, h, g, D, scale=1.0):
+    """One projection's rows [B][T][(h + 2 g) D], host bits and device columns."""
+    bits = synth.normal_bf16(seed, 0, (B, T, (h + 2 * g) * D), scale=scale)
+    dev = mlkv.bf16_tensor(bits, "cuda")
+    cut = [(0, h), (h, g), (h + g, g)]
+    return ([bits[..., a * D:(a + n) * D].reshape(B, T, n, D) for a, n in cut],
+            [dev[..., a * D:(a + n) * D].unflatten(-1, (n, D)) for a, n in cut])
+
+
+def _weight(seed, D):
+    return synth.f32_to_bf16((1 + 0.1 * synth.bf16_to_f32(synth.normal_bf16(seed, 9, (D,)))))
+
+
+def _check(got, bits, weight, eps, dims, base, pos, label):
+    ref, bound = serve_ref.norm_rope(bits, weight, eps, dims, base, pos)
+    d = np.abs(got - ref)
+    assert np.all(d <= bound), (label, np.unravel_index(np.argmax(d - bound), d.shape), d.max())
+
+
+@pytest.mark.parametrize("D,h,g,T,dims,normed", [
+    (64, 12, 1, 1, 16, True), (64, 12, 4, 45, 64, True), (64, 7, 7, 3, 48, True),
+    (128, 32, 8, 1, 128, True), (128, 8, 2, 33, 32, True), (64, 12, 3, 9, 0, True),
+    (128, 4, 1, 70, 112, False), (64, 12, 1, 8, 16, False), (64, 1, 1, 17, 0, False)])
+def test_queries_and_keys(D, h, g, T, dims, normed):
+    """Odd head counts, partial and full rotation, either step left out, columns
+    of a projection; contexts at tile edges and far positions."""
+    S = 160
+    ctx = np.array([0, 1, 31, 32, S - T], np.int32)
+    B, eps, base = ctx.size, 1e-5, 500000.0
+    label = f"norm D{D} h{h} g{g} T{T} dims{dims}"
+    say(label)
+    (q, k, v), (qd, kd, vd) = _projected(71, B, T, h, g, D, 2.0)
+    wq, wk = (_weight(s, D) if normed else None for s in (1, 2))
+    wd = [None if w is None else mlkv.bf16_tensor(w, "cuda") for w in (wq, wk)]
+    mp = mlkv.Map.uniform(4, h, 2, g)
+    cache = mlkv.Cache.empty(2 * g, B, S, D)
+    cache.k.fill_(5.0)
+    cache.v.fill_(6.0)
+    q_out = torch.empty((B, T, h, D), dtype=torch.bfloat16, device="cuda")
+    lens = torch.from_numpy(ctx).cuda()
+    mlkv.norm_rope_append(2, mp, cache, qd, kd, vd, lens, q_out, q_norm=wd[0], k_norm=wd[1],
+                          eps=eps, rotary_dims=dims, rotary_base=base)
+    pos = ctx[:, None] + np.arange(T)
+    _check(q_out.double().cpu().numpy(), q, wq, eps, dims, base, pos, label + " q")
+    rows_k, rows_v = (x.double().cpu().numpy() for x in cache.read_rows())
+    kept = np.ones((B, S), bool)
+    for b in range(B):
+        at = slice(ctx[b], ctx[b] + T)
+        kept[b, at] = False
+        _check(rows_k[g:, b, at].transpose(1, 0, 2), k[b], wk, eps, dims, base, pos[b], label + " k")
+        assert np.array_equal(rows_v[g:, b, at].transpose(1, 0, 2), serve_ref.f64(v[b]))
+    assert np.all(rows_k[:g] == 5) and np.all(rows_v[:g] == 6)
+    assert np.all(rows_k[g:][:, kept] == 5) and np.all(rows_v[g:][:, kept] == 6)
+    # The 4-bit cache holds the same bf16 rows' values, and the queries are the same.
+    four = mlkv.QCache.empty(2 * g, B, S, D)
+    four.data.fill_(0x11)
+    q_four = torch.empty_like(q_out)
+    mlkv.norm_rope_append(2, mp, four, qd, kd, vd, lens, q_four, q_norm=wd[0], k_norm=wd[1],
+                          eps=eps, rotary_dims=dims, rotary_base=base)
+    assert torch.equal(q_four, q_out)
+    two = mlkv.QCache.empty(2 * g, B, S, D)
+    two.data.fill_(0x11)
+    k_rows = torch.stack([cache.read_rows(g, g)[0][:, b, ctx[b]:ctx[b] + T] for b in range(B)], 1)
+    v_rows = vd.permute(2, 0, 1, 3).contiguous()
+    two.write_rows(k_rows.contiguous(), v_rows, g, starts=lens)
+    assert torch.equal(four.data, two.data)
+
+
+@pytest.mark.parametrize("pos", [0, 1000, 131071, 10 ** 6, 2 * 10 ** 9])
+def test_far_positions(pos):
+    """The queries of a layer without heads of its own: positions alone count,
+    up to the largest an int32 holds."""
+    D, h = 64, 3
+    (q, _, _), (qd, _, _) = _projected(72, 1, 1, h, 1, D)
+    mp = mlkv.Map.uniform(2, h, 1, 1)
+    cache = mlkv.Cache.empty(1, 1, 32, D)
+    q_out = torch.empty((1, 1, h, D), dtype=torch.bfloat16, device="cuda")
+    mlkv.norm_rope_append(1, mp, cache, qd, None, None,
+                          torch.tensor([pos], dtype=torch.int32, device="cuda"), q_out,
+                          rotary_dims=D)
+    _check(q_out.double().cpu().numpy(), q, None, 0.0, D, 10000.0, np.array([[pos]]), f"pos {pos}")
+
+
+def test_queries_in_place_and_rows_of_zeros():
+    D, h, B, T = 128, 5, 2, 11
+    (q, _, _), _ = _projected(73, B, T, h, 1, D)
+    q[0, 3] = 0
+    qd = mlkv.bf16_tensor(q, "cuda")
+    mp = mlkv.Map.uniform(2, h, 1, 1)
+    cache = mlkv.Cache.empty(1, B, 32, D)
+    ctx = torch.tensor([4, 9], dtype=torch.int32, device="cuda")
+    w = _weight(3, D)
+    mlkv.norm_rope_append(1, mp, cache, qd, None, None, ctx, qd, q_norm=mlkv.bf16_tensor(w, "cuda"),
+                          rotary_dims=64)
+    pos = np.array([[4], [9]]) + np.arange(T)
+    got = qd.double().cpu().numpy()
+    _check(got, q, w, 1e-6, 64, 10000.0, pos, "in place")
+    assert not got[0, 3].any()
+
+
+def test_slots_outside_the_cache_are_skipped():
+    D, g, S, T = 64, 1, 32, 4
+    (q, k, v), (qd, kd, vd) = _projected(74, 3, T, 2, g, D)
+    mp = mlkv.Map.uniform(2, 2, 1, g)
+    ctx = torch.tensor([-2, 30, 500], dtype=torch.int32, device="cuda")
+    for cache in (mlkv.Cache.empty(1, 3, S, D), mlkv.QCache.empty(1, 3, S, D)):
+        planes = [cache.data] if isinstance(cache, mlkv.QCache) else [cache.k, cache.v]
+        for p in planes:
+            p.fill_(3)
+        q_out = torch.empty((3, T, 2, D), dtype=torch.bfloat16, device="cuda")
+        mlkv.norm_rope_append(0, mp, cache, qd, kd, vd, ctx, q_out)
+        rows = cache.read_rows()[1].cpu()
+        before = mlkv.QCache(torch.full_like(cache.data, 3)) if isinstance(cache, mlkv.QCache) \
+            else None
+        empty = before.read_rows()[1].cpu() if before else torch.full_like(rows, 3)
+        assert torch.equal(rows[0, 0, 2:], empty[0, 0, 2:])
+        assert torch.equal(rows[0, 1, :30], empty[0, 1, :30])
+        assert torch.equal(rows[0, 2], empty[0, 2])
+        if not before:
+            assert torch.equal(rows[0, 0, :2], vd[0, 2:, 0].cpu())
+            assert torch.equal(rows[0, 1, 30:], vd[1, :2, 0].cpu())
+
+
+@pytest.mark.parametrize("D,h,g,window,sinks", [(64, 12, 1, 24, 3), (128, 8, 4, 0, 0)])
+def test_a_layer_of_a_serving_loop(D, h, g, window, sinks):
+    """A prompt of 40 tokens and ten single tokens through an owning layer and
+    one that reads its heads: norm, rotation and append, then attention, from a
+    bf16 cache and from the 4-bit cache, with the queries the calls made."""
+    say(f"serving loop D{D} w{window}")
+    B, T, S, eps = 3, 40, 96, 1e-6
+    start = np.array([0, 5, 20], np.int32)
+    mp = mlkv.Map.uniform(2, h, 1, g)
+    bf16, four = mlkv.Cache.empty(g, B, S, D), mlkv.QCache.empty(g, B, S, D)
+    bf16.k.fill_(float("nan"))
+    bf16.v.fill_(float("nan"))
+    four.data.fill_(0xFF)
+    old_k, old_v = (synth.normal_bf16(75, s, (g, B, 20, D)) for s in (1, 2))
+    zero = torch.zeros(B, dtype=torch.int32, device="cuda")
+    bf = [mlkv.bf16_tensor(x, "cuda") for x in (old_k, old_v)]
+    four.write_rows(*bf, starts=zero)  # slots up to 20 filled; a sequence attends its own
+    full = [torch.zeros((g, B, S, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for x, rows in zip(full, bf):
+        x[:, :, :20] = rows
+    bf16.write_rows(*full)
+    ws = mlkv.window_workspace(mp, B, S, D)
+    w = [mlkv.bf16_tensor(_weight(s, D), "cuda") for s in (5, 6)]
+    ctx = torch.from_numpy(start).cuda()
+
+    def values():
+        k, v = (x.double().cpu().numpy() for x in bf16.read_rows())
+        return (k, v), tuple(x.double().cpu().numpy() for x in four.read_rows())
+
+    def check(out, q, cached, n0, tokens, label):
+        q, out = q.double().cpu().numpy(), out.double().cpu().numpy()
+        G = h // g
+        for b in range(B):
+            for t in range(tokens):
+                at = serve_ref.attended(int(n0[b]) + t, window, sinks)
+                for r in range(g):
+                    hs = slice(r * G, (r + 1) * G)
+                    ref, bound = serve_ref.attend(q[b, t, hs], cached[0][r, b], cached[1][r, b], at)
+                    assert np.all(np.abs(out[b, t, hs] - ref) <= bound), (label, b, t)
+
+    for step in range(11):
+        n = T if step == 0 else 1
+        for layer in (0, 1):
+            _, (qd, kd, vd) = _projected(80 + 2 * step + layer, B, n, h, g, D)
+            new = (kd, vd) if layer == 0 else (None, None)
+            q_bf16 = torch.empty((B, n, h, D), dtype=torch.bfloat16, device="cuda")
+            q_four = torch.empty_like(q_bf16)
+            kw = dict(q_norm=w[0], k_norm=w[1], eps=eps, rotary_dims=32)
+            mlkv.norm_rope_append(layer, mp, bf16, qd, *new, ctx, q_bf16, **kw)
+            mlkv.norm_rope_append(layer, mp, four, qd, *new, ctx, q_four, **kw)
+            assert torch.equal(q_bf16, q_four)
+            cached, cached4 = values()
+            n0 = ctx.cpu().numpy()
+            out = torch.empty((B, n, h, D), dtype=torch.float32, device="cuda")
+            if n > 1:
+                mlkv.prefill_attention_window(layer, q_bf16, bf16, mp, ctx, out, window, sinks)
+                check(out, q_bf16, cached, n0, n, f"prompt layer {layer}")
+                continue
+            q1, o1 = q_bf16.view(B, h, D), out.view(B, h, D)
+            mlkv.decode_attention_window(layer, q1, bf16, mp, ctx + 1, o1, window, sinks, ws=ws)
+            check(out, q_bf16, cached, n0, 1, f"step {step} layer {layer}")
+            mlkv.qcache_decode_attention(layer, q1, four, mp, ctx + 1, o1, window, sinks, ws=ws)
+            check(out, q_bf16, cached4, n0, 1, f"step {step} layer {layer} 4-bit")
+        ctx = ctx + n

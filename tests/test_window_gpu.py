@@ -1,0 +1,275 @@
+"""Attention over the 4-bit cache and within a window, decode and prefill,
+against the plain 64-bit statement (tests/serve_ref.py), each element within
+the bound that bf16 weights and fp32 sums allow."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import serve_ref  # noqa: E402
+import synth  # noqa: E402
+from gpu_util import BOUND_MAX_POSITIONS, say  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+mlkv = pytest.importorskip("paper_2406_09297_amd")
+
+NAN = 0x7FC0
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    mlkv.lib()
+    yield
+
+
+class Case:
+    """A layer's cache, 4-bit or bf16, of two groups of g heads, the second
+    read by `layer`; slots that no sequence attends hold NaN."""
+
+    def __init__(self, four_bits, h, g, D, lens, S, seed, k_scale=1.0, T=1, window=0, sinks=0):
+        self.four_bits, self.h, self.g, self.D, self.T = four_bits, h, g, D, T
+        self.lens = np.asarray(lens, np.int32)
+        self.B, self.S, self.window, self.sinks = self.lens.size, S, window, sinks
+        self.map = mlkv.Map.uniform(4, h, 2, g)
+        shape = (g, self.B, S, D)
+        k, v = synth.normal_bf16(seed, 1, shape, scale=k_scale), synth.normal_bf16(seed, 2, shape)
+        self.attended = []
+        for b, L in enumerate(self.lens):  # positions any of the T tokens (the last: L - 1) attends
+            at = [serve_ref.attended(int(n), window, sinks) for n in range(L - T, L)]
+            self.attended.append(at)
+            off = np.setdiff1d(np.arange(S), np.concatenate(at + [np.zeros(0, int)]))
+            k[:, b, off] = NAN
+            v[:, b, off] = NAN
+        kd, vd = mlkv.bf16_tensor(k, "cuda"), mlkv.bf16_tensor(v, "cuda")
+        if four_bits:
+            self.cache = mlkv.QCache.empty(2 * g, self.B, S, D)
+            self.cache.data.fill_(0xFF)
+            self.k, self.v = serve_ref.held(k), serve_ref.held(v)
+        else:
+            self.cache = mlkv.Cache.empty(2 * g, self.B, S, D)
+            self.cache.k.fill_(float("nan"))
+            self.cache.v.fill_(float("nan"))
+            self.k, self.v = serve_ref.f64(k), serve_ref.f64(v)
+        self.cache.write_rows(kd, vd, g)
+        self.layer = 3
+        qs = (self.B, T, h, D) if T > 1 else (self.B, h, D)
+        self.q_bits = synth.normal_bf16(seed, 3, qs)
+        self.q = mlkv.bf16_tensor(self.q_bits, "cuda")
+        self.seq_lens = torch.from_numpy(self.lens).cuda()
+        self.ws = mlkv.window_workspace(self.map, self.B, S, D)
+
+    def decode(self, dtype=torch.float32, hint=0, stream=None):
+        out = torch.full(self.q.shape, 7.0, dtype=dtype, device="cuda")
+        f = mlkv.qcache_decode_attention if self.four_bits else mlkv.decode_attention_window
+        f(self.layer, self.q, self.cache, self.map, self.seq_lens, out, window=self.window,
+          sinks=self.sinks, max_len_hint=hint, ws=self.ws, stream=stream)
+        return out
+
+    def prefill(self, dtype=torch.float32):
+        out = torch.full(self.q.shape, 7.0, dtype=dtype, device="cuda")
+        mlkv.prefill_attention_window(self.layer, self.q, self.cache, self.map,
+                                      self.seq_lens - self.T, out, window=self.window,
+                                      sinks=self.sinks)
+        return out
+
+    def check(self, out, label, tokens=None):
+        G = self.h // self.g
+        out = out.double().cpu().numpy().reshape(self.B, self.T, self.h, self.D)
+        q = serve_ref.f64(self.q_bits).reshape(out.shape)
+        worst = 0.0
+        for b in range(self.B):
+            for t in range(self.T) if tokens is None else tokens:
+                at = self.attended[b][t]
+                for r in range(self.g):
+                    hs = slice(r * G, (r + 1) * G)
+                    ref, bound = serve_ref.attend(q[b, t, hs], self.k[r, b], self.v[r, b], at)
+                    d = np.abs(out[b, t, hs] - ref)
+                    if at.size > BOUND_MAX_POSITIONS:  # the bar of longer rows
+                        bound = np.full(ref.shape, 2e-3 * max(1.0, np.abs(ref).max()))
+                    assert np.all(d <= bound), (label, b, t, r, d.max(), bound.min())
+                    worst = max(worst, float((d / np.maximum(bound, 1e-300)).max(initial=0.0)))
+        say(f"  {label}: max|d|/bound={worst:.3f}")
+
+
+WINDOWS = [(0, 0), (1, 0), (1, 1), (5, 0), (32, 0), (33, 32), (31, 3), (64, 40), (100, 200),
+           (10 ** 9, 10 ** 9)]
+LENS = [0, 1, 2, 31, 32, 33, 63, 64, 65, 96, 127, 160]
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("D,h,g", [(64, 12, 1), (128, 8, 2)])
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+def test_decode_lengths_and_windows_across_tile_edges(four_bits, D, h, g, window, sinks):
+    label = f"decode {'4-bit' if four_bits else 'bf16'} D{D} w{window} s{sinks}"
+    say(label)
+    c = Case(four_bits, h, g, D, LENS, 160, 51, window=window, sinks=sinks)
+    c.check(c.decode(), label)
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 3, 16, 17, 24, 33, 70])
+def test_decode_group_sizes(four_bits, D, G):
+    """One to many query heads per KV head: one block of rows, two, and several
+    chunks; long enough for split runs."""
+    label = f"decode {'4-bit' if four_bits else 'bf16'} D{D} G{G}"
+    say(label)
+    c = Case(four_bits, 2 * G, 2, D, [700, 33, 1], 704, 52, window=0 if G % 2 else 530, sinks=4)
+    c.check(c.decode(), label)
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("D,lens,window,sinks", [
+    (64, [6000, 40, 0, 2500], 0, 0), (64, [9000], 4000, 70), (128, [3000, 2999], 0, 0),
+    (128, [5000], 2049, 1), (64, [33] * 40 + [3000], 0, 0)])
+def test_decode_split_runs(four_bits, D, lens, window, sinks):
+    """Few long sequences are cut into many runs and merged in place: within the
+    bound, the same bits every time, also from another stream and after other
+    calls on the same workspace."""
+    label = f"decode split {'4-bit' if four_bits else 'bf16'} D{D} {lens[:4]} w{window}"
+    say(label)
+    S = (max(lens) + 63) // 32 * 32
+    c = Case(four_bits, 12, 4, D, lens, S, 53, k_scale=3.0, window=window, sinks=sinks)
+    out = c.decode(hint=max(lens))
+    c.check(out, label)
+    for _ in range(5):
+        assert torch.equal(c.decode(hint=max(lens)), out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = c.decode(hint=max(lens), stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, out)
+    # The counters are left at zero for whoever uses the workspace next.
+    assert not c.ws[:262144].any() or c.ws.numel() <= 16
+    bf16 = c.decode(torch.bfloat16, hint=max(lens))
+    assert torch.equal(bf16, out.bfloat16())
+
+
+def test_lengths_above_the_hint_are_truncated_to_it():
+    c = Case(True, 12, 1, 64, [300, 100], 320, 54)
+    out = c.decode(hint=100)
+    c.attended = [[np.arange(100)], [np.arange(100)]]
+    c.check(out, "decode truncated")
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_lengths_outside_the_cache_are_clamped(four_bits):
+    c = Case(four_bits, 12, 1, 64, [64, 64], 64, 55)
+    want = c.decode()
+    c.seq_lens = torch.tensor([2 ** 31 - 1, -3], dtype=torch.int32, device="cuda")
+    got = c.decode()
+    assert torch.equal(got[0], want[0]) and not got[1].any()
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("window", [0, 40])
+def test_what_is_attended_and_not_finite_comes_through(four_bits, window):
+    """A NaN key makes its heads NaN; a value that is not finite makes its
+    channels so (in 4 bits: its block of 32); other sequences keep theirs."""
+    D = 64
+    c = Case(four_bits, 4, 1, D, [90, 90, 90, 90], 96, 56, window=window)
+    clean = c.decode()
+    k, v = (t.clone() for t in c.cache.read_rows(1, 1)[:2]) if four_bits else \
+        (t.clone() for t in c.cache.read_rows(1, 1))
+    k[0, 0, 70, 5] = float("nan")
+    v[0, 1, 70, 40] = float("inf")
+    v[0, 2, 70, 40] = float("nan")
+    c.cache.write_rows(k, v, 1)
+    out = c.decode()
+    assert out[0].isnan().all()
+    block = slice(32, 64) if four_bits else slice(40, 41)
+    rest = [d for d in range(D) if not block.start <= d < block.stop]
+    for b in (1, 2):
+        assert not out[b][:, block].isfinite().any()
+        assert torch.equal(out[b][:, rest], clean[b][:, rest])
+    assert torch.equal(out[3], clean[3])
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_decode_captured_in_a_graph_follows_the_lengths(four_bits):
+    c = Case(four_bits, 12, 4, 64, [1500, 900], 1600, 57, window=1000, sinks=5)
+    c.decode()
+    out = torch.empty(c.q.shape, dtype=torch.float32, device="cuda")
+    f = mlkv.qcache_decode_attention if four_bits else mlkv.decode_attention_window
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f(c.layer, c.q, c.cache, c.map, c.seq_lens, out, window=1000, sinks=5, ws=c.ws)
+    for lens in ([1500, 900], [1400, 1], [1500, 900], [0, 1203]):
+        # Shorter sequences only: every attended slot of theirs is filled.
+        c.cache.k.nan_to_num_(0) if not four_bits else c.cache.data.copy_(
+            torch.where(c.cache.data == 255, torch.zeros_like(c.cache.data), c.cache.data))
+        c.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        if not four_bits:
+            c.cache.v.nan_to_num_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, c.decode())
+
+
+# ------------------------------------------------------------------ prefill ---
+
+@pytest.mark.parametrize("D,h,g", [(64, 12, 1), (128, 8, 2)])
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+def test_prefill_windows_across_tile_edges(D, h, g, window, sinks):
+    T = 45
+    label = f"prefill D{D} w{window} s{sinks}"
+    say(label)
+    c = Case(False, h, g, D, [T, T + 1, T + 31, T + 32, T + 100], 160, 61, T=T, window=window,
+             sinks=sinks)
+    c.check(c.prefill(), label)
+
+
+@pytest.mark.parametrize("D,h,g,T,ctx,window,sinks", [
+    (64, 12, 12, 70, 33, 20, 2), (64, 24, 1, 2, 200, 64, 4), (64, 40, 1, 9, 10, 7, 0),
+    (128, 32, 8, 33, 500, 300, 4), (128, 16, 1, 130, 0, 50, 33), (64, 12, 1, 600, 1000, 257, 4),
+    (128, 4, 4, 300, 7, 100, 0)])
+def test_prefill_shapes(D, h, g, T, ctx, window, sinks):
+    label = f"prefill D{D} h{h} g{g} T{T} ctx{ctx} w{window} s{sinks}"
+    say(label)
+    S = (ctx + T + 63) // 32 * 32
+    c = Case(False, h, g, D, [ctx + T, T], S, 62, k_scale=3.0, T=T, window=window, sinks=sinks)
+    out = c.prefill()
+    c.check(out, label, tokens=None if T < 200 else range(0, T, 13))
+    assert torch.equal(c.prefill(), out)
+    assert torch.equal(c.prefill(torch.bfloat16), out.bfloat16())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_of_one_token_is_a_decode_step(D):
+    """T = 1 (and a window longer than the text is the plain prefill)."""
+    c = Case(False, 12, 4, D, [300, 77], 320, 63, window=90, sinks=6)
+    step = c.decode()
+    out = torch.empty((2, 1, 12, D), dtype=torch.float32, device="cuda")
+    mlkv.prefill_attention_window(c.layer, c.q.view(2, 1, 12, D), c.cache, c.map, c.seq_lens - 1,
+                                  out, window=90, sinks=6)
+    c.check(out, "prefill of one")
+    c.check(step, "decode of the same")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_values_that_are_not_finite_reach_only_who_attends_them(D):
+    """An infinite and a NaN value at position 50: tokens before it, and tokens
+    whose window has passed it, keep their results."""
+    T, window, at = 100, 20, 50
+    c = Case(False, 4, 1, D, [T], 128, 64, T=T, window=window, sinks=2)
+    clean = c.prefill()
+    k, v = (t.clone() for t in c.cache.read_rows(1, 1))
+    v[0, 0, at, 3] = float("inf")
+    v[0, 0, at, 7] = float("nan")
+    k[0, 0, 80, 1] = float("nan")  # and a key: scores of its position are NaN
+    c.cache.write_rows(k, v, 1)
+    out = c.prefill()
+    n = torch.arange(T, device="cuda")
+    hit_v, hit_k = (n >= at) & (n < at + window), (n >= 80) & (n < 80 + window)
+    assert out[0][hit_k].isnan().all()
+    rows = out[0][hit_v & ~hit_k]
+    assert not rows[..., [3, 7]].isfinite().any()
+    others = [d for d in range(D) if d not in (3, 7)]
+    want = clean[0][hit_v & ~hit_k][..., others]
+    assert torch.allclose(rows[..., others], want, rtol=1e-6, atol=1e-6)
+    free = ~hit_v & ~hit_k
+    assert torch.allclose(out[0][free], clean[0][free], rtol=1e-6, atol=1e-6)
