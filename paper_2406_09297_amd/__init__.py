@@ -156,8 +156,8 @@ def _check(status: int):
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # the handle alone: a Stream object around it costs 2 us a call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
@@ -180,6 +180,9 @@ class Map:
 
     def __init__(self, handle: int):
         self._h = ctypes.c_void_p(handle)
+        self._heads = lib().mlkv_map_num_q_heads(self._h)
+        self._owned = [max(0, lib().mlkv_map_layer_owned_count(self._h, n))
+                       for n in range(lib().mlkv_map_num_layers(self._h))]
 
     @classmethod
     def uniform(cls, l: int, h: int, m: int, g: int) -> "Map":
@@ -452,44 +455,55 @@ def prefill_step(q_all: torch.Tensor, k_new_all: torch.Tensor, v_new_all: torch.
 # Long contexts: a cache in 4 bits, attention within a window, norm and rotation
 # ---------------------------------------------------------------------------
 
+_OUT_DTYPES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
+
+
 def _out_dtype(out: torch.Tensor) -> int:
-    if out.dtype not in (torch.float32, torch.bfloat16):
+    if out.dtype not in _OUT_DTYPES:
         raise ValueError("out must be float32 or bfloat16")
-    return OUT_BF16 if out.dtype == torch.bfloat16 else OUT_F32
+    return _OUT_DTYPES[out.dtype]
 
 
-def _shaped(t: torch.Tensor, shape, name: str, dtype=torch.bfloat16) -> int:
-    """Device pointer of a contiguous tensor of exactly this shape."""
-    if tuple(t.shape) != tuple(shape):
+def _arg(t: torch.Tensor, shape, dtype, device: int, name: str) -> int:
+    """Device pointer of a contiguous tensor of this shape and type on `device`."""
+    if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return _dev_ptr(t, dtype, name)
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the cache's device, cuda:{device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _row_stride(t: torch.Tensor, name: str) -> int:
-    """Elements between the [heads][D] rows of a bf16 device tensor
-    [B][T][heads][D] whose rows lie at one distance (T rows to a sequence)."""
-    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 4:
-        raise ValueError(f"{name} must be a bfloat16 device tensor [B][T][heads][D]")
-    B, T, heads, D = t.shape
+def _rows_arg(t: torch.Tensor, shape, device: int, name: str):
+    """(device pointer, elements between rows) of a bfloat16 tensor
+    [B][T][heads][D] whose [heads][D] rows are contiguous and evenly spaced."""
+    if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device:
+        raise ValueError(f"{name} must be {tuple(shape)} in bfloat16 on cuda:{device}, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    B, T, heads, D = shape
     sb, st, sh, sd = t.stride()
     row = st if T > 1 else sb if B > 1 else heads * D
-    if (D > 1 and sd != 1) or (heads > 1 and sh != D) or (B > 1 and sb != T * row):
+    if sd != 1 or (heads > 1 and sh != D) or (B > 1 and sb != T * row):
         raise ValueError(f"{name}: rows must be contiguous and evenly spaced, strides {t.stride()}")
-    return row
+    return t.data_ptr(), row
 
 
-def _on_device(device: torch.device, *tensors):
-    """The tensors' device must be the current one: kernels are launched there."""
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {t.device} and {device}")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {device}, current device {torch.cuda.current_device()}")
+def _launch_device(device: int) -> int:
+    """The cache's device, which must be the current one: kernels are launched there."""
+    if device != torch.cuda.current_device():
+        raise ValueError(f"tensors on cuda:{device}, current device {torch.cuda.current_device()}")
+    return device
 
 
-def _ws_args(ws):
-    return (None, 0) if ws is None else (_dev_ptr(ws, ws.dtype, "ws"),
-                                         ws.numel() * ws.element_size())
+def _ws_args(ws, device: int):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on cuda:{device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 class QCache:
@@ -518,61 +532,68 @@ class QCache:
     def struct(self):
         return ctypes.byref(self._c)
 
-    def _starts(self, starts):
-        if starts is None:
-            return None
-        return _shaped(starts, (self.batch,), "starts", torch.int32)
+    def _rows(self, starts, n: int, T: int):
+        """(device, starts pointer, row shape) of a conversion."""
+        device = _launch_device(self.data.get_device())
+        at = None if starts is None else _arg(starts, (self.batch,), torch.int32, device, "starts")
+        return device, at, (n, self.batch, T, self.head_dim)
 
     def write_rows(self, k_rows: torch.Tensor, v_rows: torch.Tensor, kv_begin: int = 0,
                    starts: torch.Tensor | None = None, stream=None):
         """mlkv_qcache_write_rows: bf16 rows [n][B][T][D] into KV heads kv_begin ..
         kv_begin + n - 1, row t of sequence b at slot starts[b] + t (default: t)."""
-        _on_device(self.data.device, k_rows, v_rows, starts)
-        n, _, T, _ = k_rows.shape
-        shape = (n, self.batch, T, self.head_dim)
-        _check(lib().mlkv_qcache_write_rows(self.struct, kv_begin, n, self._starts(starts), T,
-                                            _shaped(k_rows, shape, "k_rows"),
-                                            _shaped(v_rows, shape, "v_rows"), _stream(stream)))
+        n, T = k_rows.shape[0], k_rows.shape[2]
+        device, at, shape = self._rows(starts, n, T)
+        _check(lib().mlkv_qcache_write_rows(
+            self.struct, kv_begin, n, at, T, _arg(k_rows, shape, torch.bfloat16, device, "k_rows"),
+            _arg(v_rows, shape, torch.bfloat16, device, "v_rows"), _stream(stream)))
 
     def read_rows(self, kv_begin: int = 0, kv_count: int | None = None,
                   starts: torch.Tensor | None = None, T: int | None = None, stream=None):
         """mlkv_qcache_read_rows: the values held, as rows (k, v), each bf16
         [kv_count][B][T][D]; T defaults to the capacity."""
-        _on_device(self.data.device, starts)
         n = self.n_kv - kv_begin if kv_count is None else kv_count
         T = self.capacity if T is None else T
-        shape = (n, self.batch, T, self.head_dim)
-        k = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
-        v = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
+        _, at, shape = self._rows(starts, n, T)
+        k, v = torch.empty((2, *shape), dtype=torch.bfloat16, device=self.data.device).unbind()
         if isinstance(stream, torch.cuda.Stream):  # the rows are written there
             k.record_stream(stream)
-            v.record_stream(stream)
-        _check(lib().mlkv_qcache_read_rows(self.struct, kv_begin, n, self._starts(starts), T,
-                                           k.data_ptr(), v.data_ptr(), _stream(stream)))
+        _check(lib().mlkv_qcache_read_rows(self.struct, kv_begin, n, at, T, k.data_ptr(),
+                                           v.data_ptr(), _stream(stream)))
         return k, v
+
+
+def _cache_of(cache):
+    """The ctypes structure and the device of a Cache or QCache."""
+    return cache.struct, _launch_device(cache.data.get_device() if isinstance(cache, QCache)
+                                        else cache.k.get_device())
+
+
+def _new_rows(layer: int, map_: Map, cache, k_new, v_new, T: int, device: int):
+    """Pointers and row stride of a layer's T new keys and values."""
+    shape = (cache.batch, T, map_._owned[layer], cache.head_dim)
+    k, stride = _rows_arg(k_new, shape, device, "k_new")
+    v, v_stride = _rows_arg(v_new, shape, device, "v_new")
+    if v_stride != stride:
+        raise ValueError("k_new and v_new must have rows at the same distance")
+    return k, v, stride
+
+
+def _check_layer(layer: int, map_: Map):
+    if not 0 <= layer < len(map_._owned):
+        raise ValueError(f"layer {layer} out of range")
 
 
 def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor,
                        v_new: torch.Tensor, ctx_lens: torch.Tensor, stream=None):
     """mlkv_qcache_append_rows: k_new/v_new [B][T][owned][D] (rows may be columns
     of a wider tensor's), stored at slots ctx_lens[b] + t."""
-    _on_device(cache.data.device, k_new, v_new, ctx_lens)
-    stride = _new_rows(layer, map_, cache, k_new, v_new)
-    _check(lib().mlkv_qcache_append_rows(layer, map_.handle, cache.struct, k_new.data_ptr(),
-                                         v_new.data_ptr(), k_new.shape[1], stride,
-                                         _shaped(ctx_lens, (cache.batch,), "ctx_lens", torch.int32),
-                                         _stream(stream)))
-
-
-def _new_rows(layer: int, map_: Map, cache, k_new: torch.Tensor, v_new: torch.Tensor) -> int:
-    """The row stride of a layer's new keys and values."""
-    shape = (cache.batch, k_new.shape[1], map_.layer_owned(layer)[1], cache.head_dim)
-    stride = _row_stride(k_new, "k_new")
-    if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape:
-        raise ValueError(f"k_new and v_new must be {shape}")
-    if _row_stride(v_new, "v_new") != stride:
-        raise ValueError("k_new and v_new must have rows at the same distance")
-    return stride
+    _check_layer(layer, map_)
+    struct, device = _cache_of(cache)
+    k, v, stride = _new_rows(layer, map_, cache, k_new, v_new, k_new.shape[1], device)
+    _check(lib().mlkv_qcache_append_rows(
+        layer, map_.handle, struct, k, v, k_new.shape[1], stride,
+        _arg(ctx_lens, (cache.batch,), torch.int32, device, "ctx_lens"), _stream(stream)))
 
 
 def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda",
@@ -584,14 +605,14 @@ def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device
     return ws
 
 
-def _window_attention(f, layer, q, cache, device, map_, seq_lens, out, window, sinks, max_len_hint,
-                      ws, stream):
-    _on_device(device, q, seq_lens, out, ws)
-    shape = (cache.batch, map_.h, cache.head_dim)
-    _check(f(layer, _shaped(q, shape, "q"), cache.struct, map_.handle,
-             _shaped(seq_lens, (cache.batch,), "seq_lens", torch.int32), window, sinks,
-             _shaped(out, shape, "out", out.dtype), _out_dtype(out), max_len_hint, *_ws_args(ws),
-             _stream(stream)))
+def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, max_len_hint, ws,
+                      stream):
+    struct, device = _cache_of(cache)
+    shape = (cache.batch, map_._heads, cache.head_dim)
+    _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), struct, map_.handle,
+             _arg(seq_lens, shape[:1], torch.int32, device, "seq_lens"), window, sinks,
+             _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint,
+             *_ws_args(ws, device), _stream(stream)))
 
 
 def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Map,
@@ -600,8 +621,8 @@ def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Ma
                             ws: torch.Tensor | None = None, stream=None):
     """mlkv_qcache_decode_attention: q [B][h][D] bf16 over the 4-bit cache ->
     out [B][h][D] (fp32 or bf16); ws from window_workspace."""
-    _window_attention(lib().mlkv_qcache_decode_attention, layer, q, cache, cache.data.device, map_,
-                      seq_lens, out, window, sinks, max_len_hint, ws, stream)
+    _window_attention(lib().mlkv_qcache_decode_attention, layer, q, cache, map_, seq_lens, out,
+                      window, sinks, max_len_hint, ws, stream)
 
 
 def decode_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Map,
@@ -610,8 +631,8 @@ def decode_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Map
                             ws: torch.Tensor | None = None, stream=None):
     """mlkv_decode_attention_window: the newest `window` positions and the
     first `sinks`; ws from window_workspace."""
-    _window_attention(lib().mlkv_decode_attention_window, layer, q, cache, cache.k.device, map_,
-                      seq_lens, out, window, sinks, max_len_hint, ws, stream)
+    _window_attention(lib().mlkv_decode_attention_window, layer, q, cache, map_, seq_lens, out,
+                      window, sinks, max_len_hint, ws, stream)
 
 
 def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Map,
@@ -619,12 +640,12 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
                              sinks: int = 0, stream=None):
     """mlkv_prefill_attention_window: q [B][T][h][D] bf16 -> out [B][T][h][D]
     (fp32 or bf16); token t of sequence b stands at position ctx_lens[b] + t."""
-    _on_device(cache.k.device, q, ctx_lens, out)
-    shape = (cache.batch, q.shape[1], map_.h, cache.head_dim)
+    struct, device = _cache_of(cache)
+    shape = (cache.batch, q.shape[1], map_._heads, cache.head_dim)
     _check(lib().mlkv_prefill_attention_window(
-        layer, _shaped(q, shape, "q"), cache.struct, map_.handle,
-        _shaped(ctx_lens, (cache.batch,), "ctx_lens", torch.int32), shape[1], window, sinks,
-        _shaped(out, shape, "out", out.dtype), _out_dtype(out), _stream(stream)))
+        layer, _arg(q, shape, torch.bfloat16, device, "q"), struct, map_.handle,
+        _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
+        _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _stream(stream)))
 
 
 def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch.Tensor | None,
@@ -638,28 +659,25 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
     and values [B][T][owned][D] stored at slots ctx_lens[b] + t (k_new and v_new
     None where the layer owns no head).  q, k_new and v_new may be columns of
     one projection's rows."""
-    four_bits = isinstance(cache, QCache)
-    device = cache.data.device if four_bits else cache.k.device
-    _on_device(device, q, k_new, v_new, ctx_lens, q_out, q_norm, k_norm)
-    B, T, h, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
-    if (B, h, D) != (cache.batch, map_.h, cache.head_dim):
-        raise ValueError(f"q must be [{cache.batch}][T][{map_.h}][{cache.head_dim}]")
+    _check_layer(layer, map_)
+    struct, device = _cache_of(cache)
+    B, T, h, D = cache.batch, q.shape[1], map_._heads, cache.head_dim
+    qp, q_stride = _rows_arg(q, (B, T, h, D), device, "q")
     kp = vp = None
     stride = 0
-    if map_.layer_owned(layer)[1]:
+    if map_._owned[layer]:
         if k_new is None or v_new is None:
             raise ValueError(f"layer {layer} owns KV heads: k_new and v_new are needed")
-        stride = _new_rows(layer, map_, cache, k_new, v_new)
-        if k_new.shape[1] != T:
-            raise ValueError(f"q has {T} tokens, k_new {k_new.shape[1]}")
-        kp, vp = k_new.data_ptr(), v_new.data_ptr()
-    weights = [None if w is None else _shaped(w, (D,), name)
-               for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
-    nr = _NormRope(*weights, float(eps), rotary_dims, float(rotary_base))
-    f = lib().mlkv_qcache_norm_rope_append if four_bits else lib().mlkv_norm_rope_append
-    _check(f(layer, map_.handle, cache.struct, q.data_ptr(), _row_stride(q, "q"), kp, vp, stride, T,
-             _shaped(ctx_lens, (B,), "ctx_lens", torch.int32), ctypes.byref(nr),
-             _shaped(q_out, (B, T, h, D), "q_out"), _stream(stream)))
+        kp, vp, stride = _new_rows(layer, map_, cache, k_new, v_new, T, device)
+    nr = _NormRope(
+        None if q_norm is None else _arg(q_norm, (D,), torch.bfloat16, device, "q_norm"),
+        None if k_norm is None else _arg(k_norm, (D,), torch.bfloat16, device, "k_norm"),
+        eps, rotary_dims, rotary_base)
+    L = lib()
+    f = L.mlkv_qcache_norm_rope_append if isinstance(cache, QCache) else L.mlkv_norm_rope_append
+    _check(f(layer, map_.handle, struct, qp, q_stride, kp, vp, stride, T,
+             _arg(ctx_lens, (B,), torch.int32, device, "ctx_lens"), ctypes.byref(nr),
+             _arg(q_out, (B, T, h, D), torch.bfloat16, device, "q_out"), _stream(stream)))
 
 
 # ---------------------------------------------------------------- model ---

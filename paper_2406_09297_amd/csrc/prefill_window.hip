@@ -13,6 +13,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "prefill.h"
 #include "serve.h"
@@ -22,37 +24,94 @@ namespace mlkv {
 
 namespace {
 
+// Four operands 1 KB apart in LDS.  Written out, since the compiler waits for
+// every direct load on its way before it reads LDS; here the kernel's own waits
+// and barriers say what has landed.
+__device__ __forceinline__ void lds_read4(const uint16_t* at, u16x8 (&op)[4]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t off = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint16_t*)at));
+  asm volatile(
+      "ds_read_b128 %0, %4\n\t"
+      "ds_read_b128 %1, %4 offset:1024\n\t"
+      "ds_read_b128 %2, %4 offset:2048\n\t"
+      "ds_read_b128 %3, %4 offset:3072\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(op[0]), "=&v"(op[1]), "=&v"(op[2]), "=&v"(op[3])
+      : "v"(off)
+      : "memory");
+#endif
+}
+
+// A 32-token tile in LDS, staged and read as by TileRing.
+template <int D>
+struct TileBuffer {
+  static constexpr int kLoads = 2 * (D / 64);  // of each wave, for a tile
+  alignas(16) uint16_t k[kTile * D];
+  alignas(16) uint16_t v[kTile * D];
+
+  __device__ __forceinline__ void issue(const uint16_t* kbase, const uint16_t* vbase, int t0) {
+    const unsigned lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned voff = (lane >> 2) * 64 + (((lane & 3) ^ vswz16(lane >> 2)) * 16);
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u) {
+      const int piece = u * 4 + wave;
+      const size_t at = static_cast<size_t>(t0) * D * 2 + piece * 1024;
+      load_lds16(reinterpret_cast<const char*>(kbase) + at, lane * 16, &k[piece * 512]);
+      load_lds16(reinterpret_cast<const char*>(vbase) + at, voff, &v[piece * 512]);
+    }
+  }
+  // Key operands of score block sb, k-steps 0 .. D/32 - 1; D = 64: both blocks
+  // in one go (sb 0).
+  __device__ __forceinline__ void read_k(u16x8 (&op)[4], int sb, int lane) const {
+    lds_read4(&k[sb * 2048 + lane * 8], op);
+  }
+  // Value operands of the output blocks 4 n .. 4 n + 3.
+  __device__ __forceinline__ void read_v(u16x8 (&op)[4], int n, int col, int grp) const {
+    lds_read4(&v[(col * 4 + (grp ^ vswz16(col))) * 8 + n * 2048], op);  // channel 16 db + col
+  }
+};
+
+// Wait until at most `n` of this wave's vector memory loads are in flight.
+template <int n>
+__device__ __forceinline__ void wait_loads_but() {
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+}
+
 // What one column (query row) attends: p <= n with p < sinks or p >= lo.
 struct Reach {
   int n, lo;
   __device__ __forceinline__ bool has(int p, int sinks) const {
     return p <= n && (p < sinks || p >= lo);
   }
-  // Bit e: position first + e (0 .. 7), from what remains up to each bound.
-  __device__ __forceinline__ unsigned bits(int first, int sinks) const {
-    return below(n + 1 - first) & (below(sinks - first) | ~below(lo - first));
-  }
-  __device__ __forceinline__ static unsigned below(int count) {  // bits 0 .. count - 1 of eight
-    return (1u << min(max(count, 0), 8)) - 1;
+  __device__ __forceinline__ static int below(int count) {  // bits 0 .. count - 1 of eight
+    return (1 << min(max(count, 0), 8)) - 1;
   }
 };
 
-__device__ __forceinline__ bool not_finite(u16x8 x) {
-  bool odd = false;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Of eight values those whose bit is set, zero for the others.
+__device__ __forceinline__ u16x8 keep_filled(u16x8 v, int filled) {
+  u32x4 d = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) odd |= (x[e] & 0x7F80) == 0x7F80;
-  return odd;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = static_cast<uint32_t>((filled << (31 - 2 * i)) >> 31) & 0xFFFFu;
+    const uint32_t hi = static_cast<uint32_t>((filled << (30 - 2 * i)) >> 31) & 0xFFFF0000u;
+    d[i] &= lo | hi;
+  }
+  return __builtin_bit_cast(u16x8, d);
 }
 
-// acc += V^T P^T token by token, each only into the columns that attend it: a
-// value that is not finite times the weight 0 of another column would make that
-// column NaN.  For the rare tiles that hold such values.
+// acc += V^T P^T (output blocks 4 n .. 4 n + 3) token by token, each only into
+// the columns that attend it: a value that is not finite times the weight 0 of
+// another column would make that column NaN.
 template <int D, int NB>
-__device__ __forceinline__ void add_values_apart(WaveState<D> (&st)[NB], const Tile<D>& t,
+__device__ __forceinline__ void add_values_apart(WaveState<D> (&st)[NB], const u16x8 (&v)[4], int n,
                                                  const bf16x8 (&pf)[NB],
                                                  const Reach (&reach)[NB], int t0, int grp,
                                                  int sinks) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma nounroll
   for (int u = 0; u < kTile; ++u) {
     u32x4 only;  // of an operand's eight tokens: token u
@@ -64,115 +123,174 @@ __device__ __forceinline__ void add_values_apart(WaveState<D> (&st)[NB], const T
       const bf16x8 w = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, pf[c]) & only);
       const bool has = reach[c].has(t0 + u, sinks);
 #pragma unroll
-      for (int db = 0; db < Tile<D>::DB; ++db) {
-        const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, t.v[db]) & only);
-        const f32x4 add = mfma_bf16(v, w, f32x4{0.f, 0.f, 0.f, 0.f});
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 one = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v[j]) & only);
+        const f32x4 add = mfma_bf16(one, w, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int i = 0; i < 4; ++i) st[c].acc[db][i] += has ? add[i] : 0.f;
+        for (int i = 0; i < 4; ++i) st[c].acc[4 * n + j][i] += has ? add[i] : 0.f;
       }
     }
   }
 }
 
-// One 32-token tile against the wave's NB blocks of 16 rows.  MASK: some row
-// does not attend some position of it.
-template <int D, int NB, bool MASK>
-__device__ __forceinline__ void window_tile(WaveState<D> (&st)[NB], Tile<D>& t,
-                                            const bf16x8 (&qf)[NB][Tile<D>::KK], int t0, int L,
-                                            const Reach (&reach)[NB], int sinks, int grp,
-                                            float scale_log2) {
-  constexpr int KK = Tile<D>::KK, DB = Tile<D>::DB;
-  float x[NB][8];
+// Scores of a tile for the wave's NB blocks of 16 rows: x[c][e] of token 8 grp + e.
+template <int D, int NB>
+__device__ __forceinline__ void window_scores(float (&x)[NB][8], const TileBuffer<D>* tile,
+                                              const bf16x8 (&qf)[NB][Tile<D>::KK], int lane) {
+  u16x8 k[4];
+  if constexpr (D == 64) tile->read_k(k, 0, lane);
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      s0 = mfma_bf16(as_bf16(t.k[0][kk]), qf[c][kk], s0);
-      s1 = mfma_bf16(as_bf16(t.k[1][kk]), qf[c][kk], s1);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[c][i] = s0[i];
-      x[c][4 + i] = s1[i];
-    }
-  }
-  const int first = t0 + grp * 8;
-  unsigned kept[NB];  // bit e: the row attends position first + e
-  bool apart = false;
-  if (MASK) {
-    bool odd = false;
-#pragma unroll
-    for (int c = 0; c < NB; ++c) kept[c] = reach[c].bits(first, sinks);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-#pragma unroll
-      for (int c = 0; c < NB; ++c) x[c][e] = (kept[c] >> e) & 1 ? x[c][e] : -INFINITY;
-      if (first + e >= L) {  // slots not filled yet may hold anything
-#pragma unroll
-        for (int db = 0; db < DB; ++db) t.v[db][e] = 0;
-      }
-    }
-#pragma unroll
-    for (int db = 0; db < DB; ++db) odd |= not_finite(t.v[db]);
-    apart = __ballot(odd) != 0;
-  }
-  // The reference of a row's weights is moved only when a tile exceeds it by
-  // more than kLazyRescale; a row that has attended nothing yet has -inf.
-  bool over = false;
-#pragma unroll
-  for (int c = 0; c < NB; ++c) over |= max8(x[c]) * scale_log2 > st[c].m + kLazyRescale;
-  if (__ballot(over)) {
+  for (int sb = 0; sb < 2; ++sb) {
+    if constexpr (D == 128) tile->read_k(k, sb, lane);
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
-      const float lmax = max8(x[c]);
-      float cm = fmaxf(lmax, __shfl_xor(lmax, 16));
-      cm = fmaxf(cm, __shfl_xor(cm, 32)) * scale_log2;
-      const float m_new = cm > st[c].m + kLazyRescale ? cm : st[c].m;
-      const float alpha = m_new == st[c].m ? 1.f : fast_exp2(st[c].m - m_new);
-      st[c].m = m_new;
-      st[c].den *= alpha;
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int db = 0; db < DB; ++db) st[c].acc[db] *= alpha;
+      for (int kk = 0; kk < Tile<D>::KK; ++kk)
+        s = mfma_bf16(as_bf16(k[D == 64 ? 2 * sb + kk : kk]), qf[c][kk], s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[c][4 * sb + i] = s[i];
     }
   }
-  const u16x8 ones = {0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80};
-  bf16x8 pf[NB];
+}
+
+// Scores to weights.  A row's weights are taken against a reference that is its
+// maximum in the first tile of which it attends something (until then its
+// denominator is zero) and is moved only when a tile exceeds it by more than
+// kLazyRescale.
+template <int D, int NB>
+__device__ __forceinline__ void window_weights(WaveState<D> (&st)[NB], float (&x)[NB][8],
+                                               float scale_log2, bf16x8 (&pf)[NB]) {
+  // x = scaled score - reference (log2 units): the weights' exponents.
+  bool move = false;
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     const float neg_m = -st[c].m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[c][e] = fmaf(x[c][e], scale_log2, neg_m);
+    move |= max8(x[c]) > kLazyRescale || st[c].den[0] == 0.f;
+  }
+  if (__ballot(move)) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      float top = max8(x[c]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const bool raise = top > kLazyRescale || (st[c].den[0] == 0.f && top > -INFINITY);
+      const float d = raise ? top : 0.f;
+      const float alpha = st[c].den[0] == 0.f ? 1.f : fast_exp2(-d);
+      st[c].m += d;
+      st[c].den *= alpha;
+#pragma unroll
+      for (int db = 0; db < Tile<D>::DB; ++db) st[c].acc[db] *= alpha;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[c][e] -= d;
+    }
+  }
+  const u16x8 ones = {0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80};
+#pragma unroll
+  for (int c = 0; c < NB; ++c) {
     u16x8 pbits;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float y = fmaf(x[c][e], scale_log2, neg_m);
-      // A masked score against a reference of -inf would be NaN.
-      if (MASK) y = (kept[c] >> e) & 1 ? y : -INFINITY;
-      pbits[e] = f32_to_bf16_bits(fast_exp2(y));
-    }
+    for (int e = 0; e < 8; ++e) pbits[e] = f32_to_bf16_bits(fast_exp2(x[c][e]));
     pf[c] = as_bf16(pbits);
     st[c].den = mfma_bf16(as_bf16(ones), pf[c], st[c].den);
   }
-  if (MASK && apart) {
-    add_values_apart<D, NB>(st, t, pf, reach, t0, grp, sinks);
-    return;
+}
+
+// What a wave needs to know of its place.
+template <int NB>
+struct WindowWave {
+  Reach reach[NB];         // of this lane's rows
+  Reach first, last;       // of the wave's first and last row
+  bool active;
+  int col, grp, L, sinks;  // L: filled positions
+  float scale_log2;
+};
+
+// One tile: the tile at next_t0 is requested into `next`, and the wave's rows
+// take the tile at t0 from `tile`.
+template <int D, int NB, bool APART>
+__device__ __forceinline__ void window_step(WaveState<D> (&st)[NB],
+                                            const TileBuffer<D>* tile,
+                                            TileBuffer<D>* next,
+                                            const uint16_t* kbase, const uint16_t* vbase, int t0,
+                                            int next_t0, const bf16x8 (&qf)[NB][Tile<D>::KK],
+                                            const WindowWave<NB>& w) {
+  next->issue(kbase, vbase, next_t0);
+  // Some row of the wave attends some of it?
+  if (!w.active || t0 > w.last.n || (t0 >= w.sinks && t0 + kTile <= w.first.lo)) return;
+  const int first = t0 + w.grp * 8;
+  float x[NB][8];
+  bf16x8 pf[NB];
+  window_scores<D, NB>(x, tile, qf, w.grp * 16 + w.col);
+  // Positions that some rows do not attend: behind the last one of a row, and
+  // between the first tokens and a row's window.
+  const bool ends = t0 + kTile - 1 > w.first.n;
+  const bool starts = t0 + kTile > w.sinks && t0 < w.last.lo;
+  if (ends) {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      const int left = w.reach[c].n + 1 - first;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[c][e] = e < left ? x[c][e] : -INFINITY;
+    }
   }
+  if (starts) {
+    if (t0 >= w.sinks) {
 #pragma unroll
-  for (int c = 0; c < NB; ++c)
+      for (int c = 0; c < NB; ++c) {
+        const int before = w.reach[c].lo - first;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-      st[c].acc[db] = mfma_bf16(as_bf16(t.v[db]), pf[c], st[c].acc[db]);
+        for (int e = 0; e < 8; ++e) x[c][e] = e >= before ? x[c][e] : -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NB; ++c) {
+        const int before = w.reach[c].lo - first, early = w.sinks - first;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[c][e] = e >= before || e < early ? x[c][e] : -INFINITY;
+      }
+    }
+  }
+  window_weights<D, NB>(st, x, w.scale_log2, pf);
+  const int filled = Reach::below(w.L - first);
+  const bool apart = APART && (ends || starts);
+#pragma unroll
+  for (int n = 0; n < Tile<D>::DB / 4; ++n) {
+    u16x8 v[4];
+    tile->read_v(v, n, w.col, w.grp);
+    if (t0 + kTile > w.L) {  // slots not filled yet may hold anything
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = keep_filled(v[i], filled);
+    }
+    if (apart) {
+      add_values_apart<D, NB>(st, v, n, pf, w.reach, t0, w.grp, w.sinks);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NB; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          st[c].acc[4 * n + i] = mfma_bf16(as_bf16(v[i]), pf[c], st[c].acc[4 * n + i]);
+    }
+  }
+}
+
+// n / d for 0 <= n < 2^31 with inv = (2^32 - 1) / d: the estimate is at most one short.
+__device__ __forceinline__ int quotient(int n, int d, uint32_t inv) {
+  const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(n), inv));
+  return n - q * d >= d ? q + 1 : q;
 }
 
 template <int D, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3)))
 void window_kernel(WindowPrefillParams p) {
   constexpr int KK = Tile<D>::KK, DB = Tile<D>::DB;
   constexpr int WAVE_ROWS = 16 * NB;
-  __shared__ TileRing<D> rg;
+  constexpr int RING = D == 64 ? 4 : 3;  // tiles in LDS: one in use, the others on their way
+  __shared__ TileBuffer<D> ring[RING];
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
-  const int col = lane & 15;
-  const int grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int unit = blockIdx.x;
   const int b = unit / p.n_groups;
   const int r = unit - b * p.n_groups;
@@ -180,74 +298,103 @@ void window_kernel(WindowPrefillParams p) {
   const int blk = gridDim.y - 1 - blockIdx.y;
   const int wg_row0 = blk * 4 * WAVE_ROWS;  // < rows: the grid has no empty workgroup
   const int row0 = wg_row0 + wave * WAVE_ROWS;
-  const bool active = row0 < rows;  // a wave past the end still stages tiles and syncs
   const int c0 = min(max(p.ctx[b], 0), p.S - 1);
-  const int L = min(c0 + p.T, p.S);  // filled positions of the sequence
   // Position and window start of a row.
   auto reach_of = [&](int rho) {
     Reach at;
-    at.n = min(c0 + min(rho, rows - 1) / p.G, p.S - 1);
+    at.n = min(c0 + quotient(min(rho, rows - 1), p.G, p.inv_G), p.S - 1);
     at.lo = p.window > 0 ? max(at.n - p.window + 1, 0) : 0;
     return at;
   };
+  // Its place in q and out: head r G + rho % G of token rho / G.
+  auto offset_of = [&](int rho) {
+    rho = min(rho, rows - 1);
+    const int tok = quotient(rho, p.G, p.inv_G);
+    return ((static_cast<size_t>(b) * p.T + tok) * p.h + r * p.G + (rho - tok * p.G)) * D;
+  };
   const Reach wg_first = reach_of(wg_row0), wg_last = reach_of(wg_row0 + 4 * WAVE_ROWS - 1);
-  const Reach w_first = reach_of(row0), w_last = reach_of(row0 + WAVE_ROWS - 1);
+  WindowWave<NB> w;
+  w.active = row0 < rows;  // a wave past the end still stages tiles and syncs
+  w.first = reach_of(row0);
+  w.last = reach_of(row0 + WAVE_ROWS - 1);
+  w.col = lane & 15;
+  w.grp = lane >> 4;
+  w.L = min(c0 + p.T, p.S);
+  w.sinks = p.sinks;
+  w.scale_log2 = p.scale_log2;
   const int head = (min(p.sinks, wg_first.lo) + kTile - 1) / kTile;
   const int skip = max(wg_first.lo / kTile, head) - head;
-  const int n_tiles = wg_last.n / kTile + 1 - skip;
+  const int n_tiles = wg_last.n / kTile + 1 - skip;  // at least one
   auto start_of = [&](int it) { return (it < head ? it : it + skip) * kTile; };
 
   const size_t seq = static_cast<size_t>(p.kv_begin + r) * p.B + b;
   const uint16_t* kbase = p.k + seq * p.S * D;
   const uint16_t* vbase = p.v + seq * p.S * D;
-  rg.issue(0, kbase, vbase, start_of(0));  // every workgroup has at least one tile
 
-  Reach reach[NB];
   bf16x8 qf[NB][KK];
   WaveState<D> st[NB];
+  auto pass = [&](auto apart) {
+    // The first tiles, those past the end as repeats of the last one, so that
+    // the number of loads in flight is known.
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    const int rho = row0 + 16 * c + col;
-    const RowPlace at = row_place(p, rho, rows, b, 0, r, D);
-    reach[c] = reach_of(rho);
-    const uint16_t* qrow = p.q + at.offset + grp * 8;
+    for (int s = 0; s < RING - 1; ++s) ring[s].issue(kbase, vbase, start_of(min(s, n_tiles - 1)));
+    if (!apart.value) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const u16x8 v = load16(qrow + kk * 32);
-      const u16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-      qf[c][kk] = as_bf16(at.valid ? v : zero);
+      for (int c = 0; c < NB; ++c) {
+        const int rho = row0 + 16 * c + w.col;
+        w.reach[c] = reach_of(rho);
+        const uint16_t* qrow = p.q + offset_of(rho) + w.grp * 8;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          const u16x8 v = load16(qrow + kk * 32);
+          const u16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+          qf[c][kk] = as_bf16(rho < rows ? v : zero);
+        }
+      }
     }
-    st[c].den = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int db = 0; db < DB; ++db) st[c].acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  // Tile it sits in buffer it & 1: at the barrier this wave's direct loads have
-  // landed, so every wave's part of tile it is there, and every wave is done
-  // with tile it - 1, whose buffer then takes tile it + 1.
-  for (int it = 0; it < n_tiles; ++it) {
+    for (int c = 0; c < NB; ++c) {
+      st[c].m = 0.f;
+      st[c].den = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int db = 0; db < DB; ++db) st[c].acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Tile it sits in buffer it % RING.  At the barrier this wave's part of it
+    // has landed (all but the loads of the RING - 2 tiles after it), so every
+    // wave's has, and every wave is done with tile it - 1, whose buffer then
+    // takes tile it + RING - 1.
+    for (int it = 0; it < n_tiles; ++it) {
+      wait_loads_but<(RING - 2) * TileBuffer<D>::kLoads>();
+      __builtin_amdgcn_s_barrier();
+      window_step<D, NB, apart.value>(st, &ring[it % RING], &ring[(it + RING - 1) % RING], kbase,
+                                      vbase, start_of(it), start_of(min(it + RING - 1, n_tiles - 1)),
+                                      qf, w);
+    }
     wait_loads();
     __syncthreads();
-    if (it + 1 < n_tiles) rg.issue((it + 1) & 1, kbase, vbase, start_of(it + 1));
-    const int t0 = start_of(it);
-    // Some row of the wave attends some of it?  Every row all of it?
-    if (!active || t0 > w_last.n || (t0 >= p.sinks && t0 + kTile <= w_first.lo)) continue;
-    Tile<D> t;
-    rg.read(t, it & 1, col, grp);
-    if (t0 + kTile - 1 <= w_first.n && (t0 + kTile <= p.sinks || t0 >= w_last.lo))
-      window_tile<D, NB, false>(st, t, qf, t0, L, reach, p.sinks, grp, p.scale_log2);
-    else
-      window_tile<D, NB, true>(st, t, qf, t0, L, reach, p.sinks, grp, p.scale_log2);
-  }
+  };
+  // A first pass takes the values as finite.  Where a result is not, a second
+  // one adds the values of masked tiles token by token: a value that is not
+  // finite must not reach rows that do not attend it (0 times it is NaN).
+  pass(std::false_type{});
+  bool odd = false;
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= !(fabsf(st[c].acc[db][i]) < INFINITY);
+  if (__syncthreads_or(odd)) pass(std::true_type{});
 
   // Lane (col, grp) holds channels db*16 + 4*grp .. +3 of its row in each block.
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
-    const RowPlace at = row_place(p, row0 + 16 * c + col, rows, b, 0, r, D);
-    if (!at.valid) continue;
+    const int rho = row0 + 16 * c + w.col;
+    if (rho >= rows) continue;
+    const size_t offset = offset_of(rho) + w.grp * 4;
     const float inv = 1.f / st[c].den[0];
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-      store4(p, at.offset + db * 16 + grp * 4, st[c].acc[db] * inv);
+    for (int db = 0; db < DB; ++db) store4(p, offset + db * 16, st[c].acc[db] * inv);
   }
 }
 
@@ -255,11 +402,11 @@ void window_kernel(WindowPrefillParams p) {
 
 hipError_t launch_prefill_window(const WindowPrefillParams& p, int head_dim, hipStream_t stream,
                                  hipEvent_t start, hipEvent_t stop) {
-  const int per_wg = prefill_rows_per_workgroup(head_dim);
+  constexpr int per_wg = kWindowRows;
   const int blocks = static_cast<int>((static_cast<long>(p.T) * p.G + per_wg - 1) / per_wg);
   const dim3 grid(p.B * p.n_groups, blocks);
-  auto kernel = head_dim == 64 ? window_kernel<64, prefill_wave_blocks(64)>
-                               : window_kernel<128, prefill_wave_blocks(128)>;
+  auto kernel = head_dim == 64 ? window_kernel<64, kWindowRows / 64>
+                               : window_kernel<128, kWindowRows / 64>;
   if (start || stop)
     hipExtLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, start, stop, 0, p);
   else

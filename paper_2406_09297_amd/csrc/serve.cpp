@@ -406,7 +406,7 @@ mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_c
   if ((s = check_tokens(T, cache->capacity)) != MLKV_OK) return s;
   if ((s = check_window(window, sinks)) != MLKV_OK) return s;
   const int B = cache->batch, D = cache->head_dim, G = map->group[layer];
-  const long per_wg = mlkv::prefill_rows_per_workgroup(D);
+  const long per_wg = mlkv::kWindowRows;
   if ((static_cast<long>(T) * G + per_wg - 1) / per_wg > kMaxGridY)
     return fail(MLKV_ERR_UNSUPPORTED, "T * (query heads per KV head) = %ld rows: at most %ld",
                 static_cast<long>(T) * G, kMaxGridY * per_wg);
@@ -442,6 +442,7 @@ mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_c
   p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(D)));
   p.window = window < p.S ? window : p.S;  // larger ones say the same
   p.sinks = sinks < p.S ? sinks : p.S;
+  p.inv_G = 0xFFFFFFFFu / static_cast<uint32_t>(G);
   Profile& prof = g_profile;
   const bool timed = prof.on && prof.used < static_cast<int>(prof.start.size());
   const hipError_t err =

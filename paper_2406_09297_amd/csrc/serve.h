@@ -90,8 +90,10 @@ hipError_t launch_span(const SpanParams& p, int head_dim, hipStream_t stream, hi
 // Causal prefill attention of one layer within a window: token t of sequence b
 // stands at n = ctx[b] + t and attends positions p <= n with p < sinks or
 // p > n - window.
+constexpr int kWindowRows = 128;  // query rows of a workgroup
 struct WindowPrefillParams : PrefillParams {
   int window, sinks;
+  uint32_t inv_G;  // (2^32 - 1) / G
 };
 hipError_t launch_prefill_window(const WindowPrefillParams& p, int head_dim, hipStream_t stream,
                                  hipEvent_t start, hipEvent_t stop);

@@ -189,8 +189,19 @@ def test_norm_rope_append(four_bits, args, want):
 
 def test_binding_checks_strides():
     rows = torch.zeros((2, 3, 10, 64), dtype=torch.bfloat16)
+    shape = (2, 3, 10, 64)
+    for bad in (rows.transpose(1, 2), rows[..., :32], rows.float(), rows[:1]):
+        with pytest.raises(ValueError):
+            mlkv._rows_arg(bad, shape, rows.get_device(), "k_new")
     with pytest.raises(ValueError):  # not a device tensor
-        mlkv._row_stride(rows, "k_new")
+        mlkv._rows_arg(rows, shape, 0, "k_new")
+    wide = torch.zeros((2, 3, 1024), dtype=torch.bfloat16)[..., 64:704].unflatten(-1, (10, 64))
+    assert mlkv._rows_arg(wide, shape, -1, "q") == (wide.data_ptr(), 1024)
+    with pytest.raises(ValueError):  # sequences farther apart than their rows
+        mlkv._rows_arg(torch.zeros((2, 4, 10, 64), dtype=torch.bfloat16)[:, :3], shape, -1, "q")
+    for bad in (rows[0], rows.float(), rows.transpose(0, 1)):
+        with pytest.raises(ValueError):
+            mlkv._arg(bad, shape, torch.bfloat16, -1, "q")
     with pytest.raises(ValueError):
         mlkv.QCache.empty(1, 1, 40, 64, device="cpu")
     with pytest.raises(ValueError):
