@@ -19,6 +19,7 @@
 #include "prefill.h"
 #include "serve.h"
 #include "tile.h"
+#include "weights.h"
 
 namespace mlkv {
 
@@ -154,50 +155,6 @@ __device__ __forceinline__ void window_scores(float (&x)[NB][8], const TileBuffe
   }
 }
 
-// Scores to weights.  A row's weights are taken against a reference that is its
-// maximum in the first tile of which it attends something (until then its
-// denominator is zero) and is moved only when a tile exceeds it by more than
-// kLazyRescale.
-template <int D, int NB>
-__device__ __forceinline__ void window_weights(WaveState<D> (&st)[NB], float (&x)[NB][8],
-                                               float scale_log2, bf16x8 (&pf)[NB]) {
-  // x = scaled score - reference (log2 units): the weights' exponents.
-  bool move = false;
-#pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    const float neg_m = -st[c].m;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[c][e] = fmaf(x[c][e], scale_log2, neg_m);
-    move |= max8(x[c]) > kLazyRescale || st[c].den[0] == 0.f;
-  }
-  if (__ballot(move)) {
-#pragma unroll
-    for (int c = 0; c < NB; ++c) {
-      float top = max8(x[c]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const bool raise = top > kLazyRescale || (st[c].den[0] == 0.f && top > -INFINITY);
-      const float d = raise ? top : 0.f;
-      const float alpha = st[c].den[0] == 0.f ? 1.f : fast_exp2(-d);
-      st[c].m += d;
-      st[c].den *= alpha;
-#pragma unroll
-      for (int db = 0; db < Tile<D>::DB; ++db) st[c].acc[db] *= alpha;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[c][e] -= d;
-    }
-  }
-  const u16x8 ones = {0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80, 0x3F80};
-#pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    u16x8 pbits;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) pbits[e] = f32_to_bf16_bits(fast_exp2(x[c][e]));
-    pf[c] = as_bf16(pbits);
-    st[c].den = mfma_bf16(as_bf16(ones), pf[c], st[c].den);
-  }
-}
-
 // What a wave needs to know of its place.
 template <int NB>
 struct WindowWave {
@@ -253,7 +210,7 @@ __device__ __forceinline__ void window_step(WaveState<D> (&st)[NB],
       }
     }
   }
-  window_weights<D, NB>(st, x, w.scale_log2, pf);
+  weigh_rows<D, NB>(st, x, w.scale_log2, pf);
   const int filled = Reach::below(w.L - first);
   const bool apart = APART && (ends || starts);
 #pragma unroll
@@ -353,12 +310,7 @@ void window_kernel(WindowPrefillParams p) {
       }
     }
 #pragma unroll
-    for (int c = 0; c < NB; ++c) {
-      st[c].m = 0.f;
-      st[c].den = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int db = 0; db < DB; ++db) st[c].acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int c = 0; c < NB; ++c) clear_rows(st[c]);
     // Tile it sits in buffer it % RING.  At the barrier this wave's part of it
     // has landed (all but the loads of the RING - 2 tiles after it), so every
     // wave's has, and every wave is done with tile it - 1, whose buffer then

@@ -123,35 +123,45 @@ mlkv_status check_row_buffers(const void* k_rows, const void* v_rows) {
 
 // How a layer's (sequence, KV head) units are cut (span.hip): `chunks` parts of
 // the G query rows, runs of run_tiles tiles, at most `runs` of a unit.
+// runs: only as many as give every compute unit one workgroup of eight waves,
+// of at least two tiles a wave (us, on 256 such workgroups / 512 / 1024 of four
+// waves: 8 x 32768 tokens of four heads in 4 bits 16.0 / 17.8 / 19.1, 128 ragged
+// sequences 8.1 / 8.7 / 10.4, 4 x 16000 tokens of two heads of 128 channels
+// 11.8 / 14.9 / 15.0; runs of one tile a wave instead of two 7.0 -> 8.0 for two
+// windows of 4096).  Grids of more workgroups keep four waves: more of them are
+// resident at once (48 x 8 windows of 1023, 128 channels, bf16 43.8 / 45.3).
 struct SpanPlan {
-  int chunks, chunk_rows, runs, run_tiles;
+  int chunks, chunk_rows, runs, run_tiles, waves;
   long units;
   size_t ml, need;  // offset of the (max, denominator) pairs, bytes in all; 0 without split runs
 };
-constexpr int kSpanMinTiles = 8;     // least tiles of a run
-constexpr long kSpanGroupsPerCu = 4;  // workgroups a compute unit is given by splitting
+constexpr int kSpanMinTiles = 16;
 
-SpanPlan span_plan(const mlkv_map* map, int layer, int batch, int head_dim, int max_len, int window,
-                   int sinks) {
+SpanPlan span_plan(const mlkv_map* map, int layer, int batch, int head_dim, bool four_bits,
+                   int max_len, int window, int sinks) {
   SpanPlan pl{};
   const int G = map->group[layer];
   const int blocks = (G + 15) / 16;
   pl.units = static_cast<long>(batch) * map->kv_count[layer];
-  pl.chunks = (blocks + mlkv::kSpanMaxBlocks - 1) / mlkv::kSpanMaxBlocks;
+  const int most = mlkv::span_max_blocks(head_dim, four_bits);
+  pl.chunks = (blocks + most - 1) / most;
   pl.chunk_rows = (G + pl.chunks - 1) / pl.chunks;
   int tiles = tiles_of(max_len < 1 ? 1 : max_len);
   if (window > 0) {  // both ends of the window and the first tokens' end inside a tile
-    const long most = tiles_of(window) + 1L + (sinks + static_cast<long>(kTileTokens) - 1) / kTileTokens;
-    tiles = static_cast<int>(tiles < most ? tiles : most);
+    const long bound = tiles_of(window) + 1L + (sinks + static_cast<long>(kTileTokens) - 1) / kTileTokens;
+    tiles = static_cast<int>(tiles < bound ? tiles : bound);
   }
   const long groups = pl.units * pl.chunks;
-  long runs = kSpanGroupsPerCu * compute_units_or_fallback() / groups;
+  const long cus = compute_units_or_fallback();
+  long runs = cus / groups;
   const long longest = tiles / kSpanMinTiles;
   runs = runs < longest ? runs : longest;
   pl.runs = static_cast<int>(runs < 1 ? 1 : runs);
   pl.run_tiles = (tiles + pl.runs - 1) / pl.runs;
+  pl.waves = groups * pl.runs <= cus ? 8 : 4;
   if (pl.runs > 1) {
-    const size_t part_rows = static_cast<size_t>(groups) * pl.runs * pl.chunk_rows;
+    const int segments = (pl.runs + mlkv::kSpanSegment - 1) / mlkv::kSpanSegment;
+    const size_t part_rows = static_cast<size_t>(groups) * (pl.runs + segments) * pl.chunk_rows;
     pl.ml = kCounterSlots * sizeof(int32_t) + align_up(part_rows * head_dim * sizeof(float), 256);
     pl.need = pl.ml + part_rows * 2 * sizeof(float);
   }
@@ -178,7 +188,7 @@ mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, con
   const int max_len = max_len_hint <= 0 ? S : max_len_hint;
   window = window < S ? window : S;  // larger ones say the same
   sinks = sinks < S ? sinks : S;
-  const SpanPlan pl = span_plan(map, layer, B, D, max_len, window, sinks);
+  const SpanPlan pl = span_plan(map, layer, B, D, q4 != nullptr, max_len, window, sinks);
   // A grid has fewer than 2^32 threads.
   if (static_cast<double>(pl.units) * pl.runs * pl.chunks >= (1L << 24) - 8.0 * pl.chunks)
     return fail(MLKV_ERR_UNSUPPORTED, "%ld (sequence, KV head) units: more than one launch takes",
@@ -215,6 +225,7 @@ mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, con
   p.chunk_rows = pl.chunk_rows;
   p.runs = pl.runs;
   p.run_tiles = pl.run_tiles;
+  p.waves = pl.waves;
   p.items = static_cast<unsigned>(pl.units * pl.runs);
   p.max_len = max_len;
   p.window = window;
@@ -366,8 +377,10 @@ size_t mlkv_workspace_bytes_window(const mlkv_map* map, int batch, int capacity,
   // The most runs are those without a window at the capacity.
   size_t most = 0;
   for (int n = 0; n < map->l; ++n) {
-    const size_t need = span_plan(map, n, batch, head_dim, capacity, 0, 0).need;
-    most = need > most ? need : most;
+    for (const bool four_bits : {false, true}) {
+      const size_t need = span_plan(map, n, batch, head_dim, four_bits, capacity, 0, 0).need;
+      most = need > most ? need : most;
+    }
   }
   return most;
 }

@@ -72,18 +72,30 @@ struct SpanParams {
   const uint8_t* q4;   // 4-bit cache
   const int32_t* lens; // [B]
   void* out;           // [B][h][D] fp32 or bf16
-  int* counters;       // [units*chunks] finished runs (zero between calls)
-  float* part_acc;     // [units*chunks][runs][chunk_rows][D]
-  float* part_ml;      // [units*chunks][runs][chunk_rows][2]
+  // Of a unit's chunk, where it may have several runs: finished segments and
+  // the finished runs of each (zero between calls); partials of the runs and
+  // of the segments.
+  int* counters;       // [units*chunks][1 + segments]
+  float* part_acc;     // [units*chunks][runs + segments][chunk_rows][D]
+  float* part_ml;      // [units*chunks][runs + segments][chunk_rows][2]
   int B, h, S;
   int kv_begin, n_groups, G;
   int chunks, chunk_rows, runs, run_tiles;
+  int waves;           // of a workgroup: 4 or 8
   unsigned items;      // units * runs
   int max_len, window, sinks;
   int out_bf16;
   float scale_log2;    // log2(e) / sqrt(D)
 };
-constexpr int kSpanMaxBlocks = 2;  // blocks of 16 rows a wave takes
+// Most blocks of 16 query rows a wave takes: two share a tile's operands (us,
+// two / one: 4-bit, 600 sequences of 3000 .. 4000 tokens, 32 heads of 128 on one
+// KV head 76.6 / 84.1; bf16 of 64 channels, 900 windows of 2048, 91 / 98),
+// except two of 128 channels beside bf16 tiles, which do not fit the registers
+// (600 windows of 2048: 173 / 125; 64 of them 23.1 / 16.6).
+constexpr int span_max_blocks(int head_dim, bool four_bits) {
+  return head_dim == 128 && !four_bits ? 1 : 2;
+}
+constexpr int kSpanSegment = 8;    // runs merged by one workgroup
 hipError_t launch_span(const SpanParams& p, int head_dim, hipStream_t stream, hipEvent_t start,
                        hipEvent_t stop);
 

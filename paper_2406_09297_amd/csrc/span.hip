@@ -26,6 +26,7 @@
 #include "qcache.h"
 #include "serve.h"
 #include "tile.h"
+#include "weights.h"
 
 namespace mlkv {
 
@@ -72,72 +73,28 @@ __device__ __forceinline__ Span span_of(int len, int max_len, int window, int si
   return s;
 }
 
-// Scores of a tile (x: tokens 8 grp + e) to weights against the row's running
-// maximum; a position that is not kept weighs nothing, whatever its score.
-template <int D>
-__device__ __forceinline__ void weigh(WaveState<D>& st, float (&x)[8], bool partial, unsigned kept,
-                                      float scale_log2) {
-  if (partial) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (kept >> e) & 1 ? x[e] : -INFINITY;
-  }
-  float tmax = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                     fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  if (__ballot(tmax * scale_log2 > st.m)) {
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
-    tmax *= scale_log2;
-    const float m_new = tmax > st.m ? tmax : st.m;
-    const float alpha = fast_exp2(st.m - m_new);  // 0 on the first tile, 1 if unchanged
-    st.m = m_new;
-    st.den *= alpha;
-#pragma unroll
-    for (int db = 0; db < Tile<D>::DB; ++db) st.acc[db] *= alpha;
-  }
-  const float neg_m = -st.m;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], scale_log2, neg_m);
-  if (partial) {  // -inf against a maximum of -inf is NaN; it counts only where kept
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (kept >> e) & 1 ? x[e] : -INFINITY;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = fast_exp2(x[e]);
-}
-
-__device__ __forceinline__ bf16x8 to_bf16(const float (&x)[8]) {
-  u16x8 b;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) b[e] = f32_to_bf16_bits(x[e]);
-  return as_bf16(b);
-}
-
-__device__ __forceinline__ unsigned kept_bits(const Span& s, int first) {
+// Of a partial tile, this lane's positions first .. first + 7: a bit for each
+// that is attended, and the scores of the others to -inf (whatever they are).
+template <int NB>
+__device__ __forceinline__ unsigned mask_scores(float (&x)[NB][8], const Span& sp, int first) {
   unsigned kept = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) kept |= (s.kept(first + e) ? 1u : 0u) << e;
+  for (int e = 0; e < 8; ++e) {
+    const bool has = sp.kept(first + e);
+    kept |= (has ? 1u : 0u) << e;
+#pragma unroll
+    for (int c = 0; c < NB; ++c) x[c][e] = has ? x[c][e] : -INFINITY;
+  }
   return kept;
 }
-
-constexpr uint16_t kOne = 0x3F80;
 
 template <int D, int NB>
 __device__ __forceinline__ void span_tile(WaveState<D> (&st)[NB], Tile<D>& t,
                                           const bf16x8 (&qf)[NB][Tile<D>::KK], const Span& sp,
                                           int t0, int grp, float scale_log2) {
   constexpr int KK = Tile<D>::KK, DB = Tile<D>::DB;
-  const bool partial = sp.partial(t0);
-  unsigned kept = 0xFF;
-  if (partial) {
-    kept = kept_bits(sp, t0 + grp * 8);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (!((kept >> e) & 1)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db) t.v[db][e] = 0;
-      }
-  }
-  const u16x8 ones = {kOne, kOne, kOne, kOne, kOne, kOne, kOne, kOne};
+  float x[NB][8];
+  bf16x8 pf[NB];
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
@@ -146,64 +103,114 @@ __device__ __forceinline__ void span_tile(WaveState<D> (&st)[NB], Tile<D>& t,
       s0 = mfma_bf16(as_bf16(t.k[0][kk]), qf[c][kk], s0);
       s1 = mfma_bf16(as_bf16(t.k[1][kk]), qf[c][kk], s1);
     }
-    float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
-    weigh<D>(st[c], x, partial, kept, scale_log2);
-    const bf16x8 pf = to_bf16(x);
-    // The denominator sums the same rounded weights: a row of ones times P^T.
-    st[c].den = mfma_bf16(as_bf16(ones), pf, st[c].den);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) st[c].acc[db] = mfma_bf16(as_bf16(t.v[db]), pf, st[c].acc[db]);
+    for (int i = 0; i < 4; ++i) {
+      x[c][i] = s0[i];
+      x[c][4 + i] = s1[i];
+    }
   }
+  if (sp.partial(t0)) {
+    const unsigned kept = mask_scores<NB>(x, sp, t0 + grp * 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // values that are not attended may be anything
+      const uint32_t keep = ((kept >> (2 * i)) & 1 ? 0xFFFFu : 0u) |
+                            ((kept >> (2 * i + 1)) & 1 ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        u32x4 v = __builtin_bit_cast(u32x4, t.v[db]);
+        v[i] &= keep;
+        t.v[db] = __builtin_bit_cast(u16x8, v);
+      }
+    }
+  }
+  weigh_rows<D, NB>(st, x, scale_log2, pf);
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      st[c].acc[db] = mfma_bf16(as_bf16(t.v[db]), pf[c], st[c].acc[db]);
+}
+
+// Byte i of d as the exponent of a power of two, in one instruction (a shift
+// of the selected byte), which the compiler makes two of for bytes 0 to 2.
+template <int i>
+__device__ __forceinline__ float byte_scale(uint32_t d) {
+  uint32_t r = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t shift = 23;
+  if constexpr (i == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD "
+        "src1_sel:BYTE_0" : "=v"(r) : "v"(shift), "v"(d));
+  if constexpr (i == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD "
+        "src1_sel:BYTE_1" : "=v"(r) : "v"(shift), "v"(d));
+  if constexpr (i == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD "
+        "src1_sel:BYTE_2" : "=v"(r) : "v"(shift), "v"(d));
+  if constexpr (i == 3)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD "
+        "src1_sel:BYTE_3" : "=v"(r) : "v"(shift), "v"(d));
+#endif
+  return __builtin_bit_cast(float, r);
 }
 
 template <int D, int NB>
 __device__ __forceinline__ void span_tile(WaveState<D> (&st)[NB], Codes<D>& t,
                                           const bf16x8 (&qf)[NB][Tile<D>::KK], const Span& sp,
                                           int t0, int grp, float scale_log2) {
-  constexpr int KK = Tile<D>::KK, DB = Tile<D>::DB;
-  const bool partial = sp.partial(t0);
-  unsigned kept = 0xFF;
-  if (partial) kept = kept_bits(sp, t0 + grp * 8);
-  const u16x8 ones = {kOne, kOne, kOne, kOne, kOne, kOne, kOne, kOne};
-  f32x4 s[NB][2];
+  constexpr int KK = Tile<D>::KK;
+  float x[NB][8];
+  bf16x8 pf[NB];
+  {
+    f32x4 s[NB][2];
 #pragma unroll
-  for (int c = 0; c < NB; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < NB; ++c) s[c][0] = s[c][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 2 * KK; ++i) {
-    // The shifts leave neighbouring bytes in the sign and mantissa, which the
-    // conversion does not read.
-    const float scale = __builtin_bit_cast(
-        float, i % 4 == 3 ? t.ke[i / 4] >> 1 : t.ke[i / 4] << (23 - 8 * (i % 4)));
-    const bf16x8 k = as_bf16(dequantise8(t.k[i / 4][i % 4], scale));
+    for (int i = 0; i < 2 * KK; ++i) {
+      // The shifts leave neighbouring bytes in the sign and mantissa, which the
+      // conversion does not read.
+      const float scale = __builtin_bit_cast(
+          float, i % 4 == 3 ? t.ke[i / 4] >> 1 : t.ke[i / 4] << (23 - 8 * (i % 4)));
+      const bf16x8 k = as_bf16(dequantise8(t.k[i / 4][i % 4], scale));
 #pragma unroll
-    for (int c = 0; c < NB; ++c) s[c][i / KK] = mfma_bf16(k, qf[c][i % KK], s[c][i / KK]);
-  }
-  bf16x8 p[NB][KK];  // the weights times the value scales of each channel block
+      for (int c = 0; c < NB; ++c) s[c][i / KK] = mfma_bf16(k, qf[c][i % KK], s[c][i / KK]);
+    }
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    float x[8] = {s[c][0][0], s[c][0][1], s[c][0][2], s[c][0][3],
-                  s[c][1][0], s[c][1][1], s[c][1][2], s[c][1][3]};
-    weigh<D>(st[c], x, partial, kept, scale_log2);
-    st[c].den = mfma_bf16(as_bf16(ones), to_bf16(x), st[c].den);
+    for (int c = 0; c < NB; ++c)
 #pragma unroll
-    for (int b = 0; b < KK; ++b) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t d = t.ve[b / 2][(b % 2) * 2 + e / 4];
-        const uint32_t bits = (e % 4 == 3 ? d >> 1 : d << (23 - 8 * (e % 4))) & 0x7F800000u;
-        float f = __builtin_bit_cast(float, bits);
-        if (partial) f = (kept >> e) & 1 ? f : 0.f;
-        y[e] = x[e] * f;
+      for (int i = 0; i < 4; ++i) {
+        x[c][i] = s[c][0][i];
+        x[c][4 + i] = s[c][1][i];
       }
-      p[c][b] = to_bf16(y);
+  }
+  if (sp.partial(t0)) {
+    // Exponents that are not attended may be NaN: 0 times the weight 0 they get.
+    const unsigned kept = mask_scores<NB>(x, sp, t0 + grp * 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t bits = (kept >> (4 * i)) & 15;
+      const uint32_t keep = ((bits * 0x00204081u) & 0x01010101u) * 0xFFu;
+#pragma unroll
+      for (int b = 0; b < KK; ++b) t.ve[b / 2][(b % 2) * 2 + i] &= keep;
     }
   }
+  weigh_rows<D, NB>(st, x, scale_log2, pf);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    const bf16x8 v = as_bf16(dequantise8(t.v[db / 4][db % 4], 1.f));
+  for (int b = 0; b < KK; ++b) {  // blocks of 32 channels, two of the output each
+    const uint32_t lo = t.ve[b / 2][(b % 2) * 2], hi = t.ve[b / 2][(b % 2) * 2 + 1];
+    const float f[8] = {byte_scale<0>(lo), byte_scale<1>(lo), byte_scale<2>(lo),
+                        byte_scale<3>(lo), byte_scale<0>(hi), byte_scale<1>(hi),
+                        byte_scale<2>(hi), byte_scale<3>(hi)};
+    const bf16x8 v0 = as_bf16(dequantise8(t.v[b / 2][(2 * b) % 4], 1.f));
+    const bf16x8 v1 = as_bf16(dequantise8(t.v[b / 2][(2 * b) % 4 + 1], 1.f));
 #pragma unroll
-    for (int c = 0; c < NB; ++c) st[c].acc[db] = mfma_bf16(v, p[c][db / 2], st[c].acc[db]);
+    for (int c = 0; c < NB; ++c) {
+      u16x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = f32_to_bf16_bits(x[c][e] * f[e]);
+      st[c].acc[2 * b] = mfma_bf16(v0, as_bf16(w), st[c].acc[2 * b]);
+      st[c].acc[2 * b + 1] = mfma_bf16(v1, as_bf16(w), st[c].acc[2 * b + 1]);
+    }
   }
 }
 
@@ -221,10 +228,10 @@ void span_kernel(SpanParams p) {
   constexpr int KK = Tile<D>::KK, DB = Tile<D>::DB;
   constexpr int NT = W * 64;
   constexpr int D4 = D / 4;
-  constexpr int PF = Q4 && D * NB < 256 ? 3 : 2;  // tiles in registers: one in use, the others on their way
+  constexpr int PF = 2;  // tiles in registers: one in use, one on its way
   __shared__ SpanShared<D, NB, W> sm;
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15;
   const int grp = lane >> 4;
 
@@ -245,8 +252,8 @@ void span_kernel(SpanParams p) {
   const Span sp = span_of(p.lens[b], p.max_len, p.window, p.sinks);
   const int nb = min(max((sp.tiles + p.run_tiles - 1) / p.run_tiles, 1), p.runs);
   if (j >= nb) return;
-  const int k0 = static_cast<int>(static_cast<long>(sp.tiles) * j / nb);
-  const int k1 = static_cast<int>(static_cast<long>(sp.tiles) * (j + 1) / nb);
+  const int each = sp.tiles / nb, more = sp.tiles - each * nb;  // the first `more` take one more
+  const int k0 = j * each + min(j, more), k1 = k0 + each + (j < more ? 1 : 0);
 
   const size_t seq = static_cast<size_t>(p.kv_begin + r) * p.B + b;
   const uint16_t* kbase = Q4 ? nullptr : p.k + seq * p.S * D;
@@ -273,9 +280,7 @@ void span_kernel(SpanParams p) {
       const u16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
       qf[c][kk] = as_bf16(rr < n_rows ? v : zero);  // padded rows score zero
     }
-    st[c].den = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int db = 0; db < DB; ++db) st[c].acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    clear_rows(st[c]);
   }
 
   int it = k0 + wave;
@@ -285,11 +290,11 @@ void span_kernel(SpanParams p) {
     typename std::conditional<Q4, Codes<D>, Tile<D>>::type t[PF];
 #pragma unroll
     for (int s = 0; s < PF - 1; ++s) load(t[s], min(it + s * W, k1 - 1));
-    for (bool more = true; more;) {
+    for (bool left = true; left;) {
 #pragma unroll
       for (int s = 0; s < PF; ++s) {
         if (it >= k1) {
-          more = false;
+          left = false;
           break;
         }
         load(t[(s + PF - 1) % PF], min(it + (PF - 1) * W, k1 - 1));
@@ -302,15 +307,30 @@ void span_kernel(SpanParams p) {
   // Merge the waves through LDS; a unit of one run is finished here, another
   // leaves a partial per run.
   const size_t uc = static_cast<size_t>(unit) * p.chunks + chunk;
-  const int part_floats = p.chunk_rows * D;  // one run's partial outputs, [row][channel]
-  float* const unit_acc = nb > 1 ? p.part_acc + uc * p.runs * part_floats : nullptr;
-  float* const unit_ml = nb > 1 ? p.part_ml + uc * p.runs * p.chunk_rows * 2 : nullptr;
+  const int part_floats = p.chunk_rows * D;  // one partial's outputs, [row][channel]
+  const int segments = (p.runs + kSpanSegment - 1) / kSpanSegment;
+  const int slots = p.runs + segments;
+  float* const unit_acc = nb > 1 ? p.part_acc + uc * slots * part_floats : nullptr;
+  float* const unit_ml = nb > 1 ? p.part_ml + uc * slots * p.chunk_rows * 2 : nullptr;
   const __amdgpu_buffer_rsrc_t rsrc =
-      device_rsrc(unit_acc, nb > 1 ? static_cast<uint32_t>(nb * part_floats * 4) : 0u);
+      device_rsrc(unit_acc, nb > 1 ? static_cast<uint32_t>(slots * part_floats * 4) : 0u);
+  // Row rr, channels d .. d + 3 of partial `slot`, or of the output (slot -1).
+  auto put = [&](int slot, int rr, int d, f32x4 o, float m, float den) {
+    if (slot < 0) {
+      store4_as<D>(p.out, p.out_bf16, out_row + rr, d, normalize4(o, den));
+      return;
+    }
+    store4_device(rsrc, (slot * part_floats + rr * D + d) * 4, o);
+    if (d == 0) {
+      store_device(&unit_ml[(slot * p.chunk_rows + rr) * 2 + 0], m);
+      store_device(&unit_ml[(slot * p.chunk_rows + rr) * 2 + 1], den);
+    }
+  };
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     if (grp == 0) {
-      sm.m[wave][c * 16 + col] = st[c].m;
+      // A row of which this wave attended nothing has no reference.
+      sm.m[wave][c * 16 + col] = st[c].den[0] == 0.f ? -INFINITY : st[c].m;
       sm.l[wave][c * 16 + col] = st[c].den[0];
     }
 #pragma unroll
@@ -333,78 +353,87 @@ void span_kernel(SpanParams p) {
       wsum += f * sm.l[w][rr];
       o += f * *reinterpret_cast<const f32x4*>(&sm.acc[w][rr][d]);
     }
-    if (nb == 1) {
-      store4_as<D>(p.out, p.out_bf16, out_row + rr, d, normalize4(o, wsum));
-    } else {
-      store4_device(rsrc, (j * part_floats + rr * D + d) * 4, o);
-      if (d == 0) {
-        store_device(&unit_ml[(j * p.chunk_rows + rr) * 2 + 0], M);
-        store_device(&unit_ml[(j * p.chunk_rows + rr) * 2 + 1], wsum);
-      }
-    }
+    put(nb == 1 ? -1 : j, rr, d, o, M, wsum);
   }
   if (nb == 1) return;
 
-  // The last run of the unit to finish merges them in run order, so results
-  // do not depend on which that is.  Every other run bumped the counter after
-  // its partials completed: the device-scope loads below see them.
-  wait_stores_complete();
-  __syncthreads();
-  if (threadIdx.x == 0)
-    sm.last = __hip_atomic_fetch_add(&p.counters[uc], 1, __ATOMIC_RELAXED,
-                                     __HIP_MEMORY_SCOPE_AGENT) == nb - 1;
-  __syncthreads();
-  if (!sm.last) return;
-  constexpr int U = 8;  // runs whose partials are requested together
-  for (int idx = threadIdx.x; idx < n_rows * D4; idx += NT) {
-    const int rr = idx / D4;
-    float M = -INFINITY, den = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < nb; s0 += U) {
-      float m[U], w[U];
-      f32x4 a[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        m[u] = -INFINITY;
-        w[u] = 0.f;
-        a[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (s0 + u < nb) {
-          float* ml = &unit_ml[((s0 + u) * p.chunk_rows + rr) * 2];
-          m[u] = load_device(ml);
-          w[u] = load_device(ml + 1);
-          a[u] = load4_device(rsrc, ((s0 + u) * part_floats + idx * 4) * 4);
-        }
-      }
-      float bm = M;
-#pragma unroll
-      for (int u = 0; u < U; ++u) bm = fmaxf(bm, m[u]);
-      const float ref = merge_reference(bm);
-      const float sc = fast_exp2(M - ref);  // 0 while nothing is accumulated
-      den *= sc;
-      o *= sc;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float f = fast_exp2(m[u] - ref);
-        den += f * w[u];
-        o += f * a[u];
-      }
-      M = bm;
+  // Merge the unit's runs in two steps, each in the order of the runs, so that
+  // results do not depend on which workgroup is the last: the last of a
+  // segment of kSpanSegment runs merges it (one round trip, the segments on
+  // as many compute units), the last segment's merges the segments.
+  int* const counters = p.counters + uc * (1 + segments);
+  auto last_of = [&](int* counter, int count) -> bool {
+    // Every other one bumped the counter after its partials completed: the
+    // device-scope loads of the merge see them.
+    wait_stores_complete();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      sm.last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                count - 1;
+      if (sm.last)  // ready for the next call on this workspace
+        __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    store4_as<D>(p.out, p.out_bf16, out_row + rr, (idx - rr * D4) * 4, normalize4(o, den));
-  }
-  if (threadIdx.x == 0)  // ready for the next call on this workspace
-    __hip_atomic_store(&p.counters[uc], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return sm.last;
+  };
+  auto merge = [&](int first, int count, int into) {
+    for (int idx = threadIdx.x; idx < n_rows * D4; idx += NT) {
+      const int rr = idx / D4;
+      float M = -INFINITY, den = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int s0 = 0; s0 < count; s0 += kSpanSegment) {
+        float m[kSpanSegment], w[kSpanSegment];
+        f32x4 a[kSpanSegment];
+#pragma unroll
+        for (int u = 0; u < kSpanSegment; ++u) {
+          m[u] = -INFINITY;
+          w[u] = 0.f;
+          a[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (s0 + u < count) {
+            const int slot = first + s0 + u;
+            float* ml = &unit_ml[(slot * p.chunk_rows + rr) * 2];
+            m[u] = load_device(ml);
+            w[u] = load_device(ml + 1);
+            a[u] = load4_device(rsrc, (slot * part_floats + idx * 4) * 4);
+          }
+        }
+        float bm = M;
+#pragma unroll
+        for (int u = 0; u < kSpanSegment; ++u) bm = fmaxf(bm, m[u]);
+        const float ref = merge_reference(bm);
+        const float sc = fast_exp2(M - ref);  // 0 while nothing is accumulated
+        den *= sc;
+        o *= sc;
+#pragma unroll
+        for (int u = 0; u < kSpanSegment; ++u) {
+          const float f = fast_exp2(m[u] - ref);
+          den += f * w[u];
+          o += f * a[u];
+        }
+        M = bm;
+      }
+      put(into, rr, (idx - rr * D4) * 4, o, M, den);
+    }
+  };
+  const int seg = j / kSpanSegment, n_seg = (nb + kSpanSegment - 1) / kSpanSegment;
+  const int in_seg = min(kSpanSegment, nb - seg * kSpanSegment);
+  if (!last_of(counters + 1 + seg, in_seg)) return;
+  merge(seg * kSpanSegment, in_seg, n_seg == 1 ? -1 : p.runs + seg);
+  if (n_seg == 1 || !last_of(counters, n_seg)) return;
+  merge(p.runs, n_seg, -1);
 }
 
-template <int D, int NB>
+template <int D, int NB, bool Q4>
 hipError_t launch_span_t(const SpanParams& p, hipStream_t stream, hipEvent_t start,
                          hipEvent_t stop) {
   const dim3 grid((p.items + 7) / 8 * 8 * static_cast<unsigned>(p.chunks));
-  auto kernel = p.q4 ? span_kernel<D, NB, kWaves, true> : span_kernel<D, NB, kWaves, false>;
+  const dim3 threads(64 * p.waves);
+  auto kernel = p.waves == kWideWaves ? span_kernel<D, NB, kWideWaves, Q4>
+                                      : span_kernel<D, NB, kWaves, Q4>;
   if (start)
-    hipExtLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, start, stop, 0, p);
+    hipExtLaunchKernelGGL(kernel, grid, threads, 0, stream, start, stop, 0, p);
   else
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(kernel, grid, threads, 0, stream, p);
   return hipGetLastError();
 }
 
@@ -413,11 +442,19 @@ hipError_t launch_span_t(const SpanParams& p, hipStream_t stream, hipEvent_t sta
 hipError_t launch_span(const SpanParams& p, int head_dim, hipStream_t stream, hipEvent_t start,
                        hipEvent_t stop) {
   const bool two = p.chunk_rows > 16;
+  if (p.waves != kWaves && p.waves != kWideWaves) return hipErrorInvalidValue;
+  if (p.chunk_rows > 16 * span_max_blocks(head_dim, p.q4)) return hipErrorInvalidValue;
+  if (p.q4) {
+    if (head_dim == 64)
+      return two ? launch_span_t<64, 2, true>(p, stream, start, stop)
+                 : launch_span_t<64, 1, true>(p, stream, start, stop);
+    return two ? launch_span_t<128, 2, true>(p, stream, start, stop)
+               : launch_span_t<128, 1, true>(p, stream, start, stop);
+  }
   if (head_dim == 64)
-    return two ? launch_span_t<64, 2>(p, stream, start, stop)
-               : launch_span_t<64, 1>(p, stream, start, stop);
-  return two ? launch_span_t<128, 2>(p, stream, start, stop)
-             : launch_span_t<128, 1>(p, stream, start, stop);
+    return two ? launch_span_t<64, 2, false>(p, stream, start, stop)
+               : launch_span_t<64, 1, false>(p, stream, start, stop);
+  return launch_span_t<128, 1, false>(p, stream, start, stop);
 }
 
 }  // namespace mlkv
