@@ -74,10 +74,23 @@ struct TileBuffer {
   }
 };
 
-// Wait until at most `n` of this wave's vector memory loads are in flight.
-template <int n>
-__device__ __forceinline__ void wait_loads_but() {
-  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+// Wait until at most the loads of the `tiles` latest tiles (or of MOST, if
+// fewer) are in flight; a wave has no other vector memory loads then.
+template <int D, int MOST>
+__device__ __forceinline__ void wait_tiles_but(int tiles) {
+  constexpr int n = MOST * TileBuffer<D>::kLoads;  // vmcnt, the other counters left alone
+  if (MOST == 0 || tiles >= MOST)
+    __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+  else if constexpr (MOST > 0)
+    wait_tiles_but<D, MOST - 1>(tiles);
+}
+
+// A barrier of the workgroup without the waits that __syncthreads puts before
+// it (for every direct load); memory operations stay on their side of it.
+__device__ __forceinline__ void group_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // What one column (query row) attends: p <= n with p < sinks or p >= lo.
@@ -165,16 +178,12 @@ struct WindowWave {
   float scale_log2;
 };
 
-// One tile: the tile at next_t0 is requested into `next`, and the wave's rows
-// take the tile at t0 from `tile`.
+// The wave's rows take the tile at t0.
 template <int D, int NB, bool APART>
 __device__ __forceinline__ void window_step(WaveState<D> (&st)[NB],
-                                            const TileBuffer<D>* tile,
-                                            TileBuffer<D>* next,
-                                            const uint16_t* kbase, const uint16_t* vbase, int t0,
-                                            int next_t0, const bf16x8 (&qf)[NB][Tile<D>::KK],
+                                            const TileBuffer<D>* tile, int t0,
+                                            const bf16x8 (&qf)[NB][Tile<D>::KK],
                                             const WindowWave<NB>& w) {
-  next->issue(kbase, vbase, next_t0);
   // Some row of the wave attends some of it?
   if (!w.active || t0 > w.last.n || (t0 >= w.sinks && t0 + kTile <= w.first.lo)) return;
   const int first = t0 + w.grp * 8;
@@ -291,10 +300,9 @@ void window_kernel(WindowPrefillParams p) {
   bf16x8 qf[NB][KK];
   WaveState<D> st[NB];
   auto pass = [&](auto apart) {
-    // The first tiles, those past the end as repeats of the last one, so that
-    // the number of loads in flight is known.
 #pragma unroll
-    for (int s = 0; s < RING - 1; ++s) ring[s].issue(kbase, vbase, start_of(min(s, n_tiles - 1)));
+    for (int s = 0; s < RING - 1; ++s)
+      if (s < n_tiles) ring[s].issue(kbase, vbase, start_of(s));
     if (!apart.value) {
 #pragma unroll
       for (int c = 0; c < NB; ++c) {
@@ -312,15 +320,18 @@ void window_kernel(WindowPrefillParams p) {
 #pragma unroll
     for (int c = 0; c < NB; ++c) clear_rows(st[c]);
     // Tile it sits in buffer it % RING.  At the barrier this wave's part of it
-    // has landed (all but the loads of the RING - 2 tiles after it), so every
-    // wave's has, and every wave is done with tile it - 1, whose buffer then
-    // takes tile it + RING - 1.
+    // has landed (all but the loads of the tiles after it), so every wave's
+    // has, and every wave is done with tile it - 1, whose buffer then takes
+    // tile it + RING - 1.
     for (int it = 0; it < n_tiles; ++it) {
-      wait_loads_but<(RING - 2) * TileBuffer<D>::kLoads>();
-      __builtin_amdgcn_s_barrier();
-      window_step<D, NB, apart.value>(st, &ring[it % RING], &ring[(it + RING - 1) % RING], kbase,
-                                      vbase, start_of(it), start_of(min(it + RING - 1, n_tiles - 1)),
-                                      qf, w);
+      if constexpr (apart.value)  // (spilled registers come and go there, too)
+        wait_loads();
+      else
+        wait_tiles_but<D, RING - 2>(n_tiles - 1 - it);
+      group_barrier();
+      if (it + RING - 1 < n_tiles)
+        ring[(it + RING - 1) % RING].issue(kbase, vbase, start_of(it + RING - 1));
+      window_step<D, NB, apart.value>(st, &ring[it % RING], start_of(it), qf, w);
     }
     wait_loads();
     __syncthreads();

@@ -21,8 +21,13 @@ namespace mlkv {
 
 namespace {
 
-constexpr int kStoreThreads = 256;
-constexpr long kMaxStoreGrid = 1L << 20;  // workgroups; each takes every gridDim-th item
+
+// A grid has fewer than 2^32 threads along x: more workgroups go along y.
+constexpr unsigned kGridX = 1u << 23;
+dim3 item_grid(unsigned items) {
+  return items <= kGridX ? dim3(items) : dim3(kGridX, (items + kGridX - 1) / kGridX);
+}
+__device__ __forceinline__ unsigned item_of_block() { return blockIdx.y * kGridX + blockIdx.x; }
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t x) {
   return __builtin_bit_cast(float, static_cast<uint32_t>(x) << 16);
@@ -38,39 +43,74 @@ __device__ __forceinline__ int block_top(u16x8 x) {
   return max(top, __shfl_xor(top, 2));
 }
 
-// One row's eight channels from c0 on: divided by the row's root mean square
-// and weighted (w not null), then rotated with cs[0 .. half) = (cos, sin) of
-// the row's token, in fp32, rounded once to bf16.  All D / 8 lanes of a row
-// take part.
+// Sums over the D / 8 lanes of a row, in every lane of it: within a quad, then
+// with the other quad of eight and the other half of sixteen lanes (mirrored:
+// what is equal in all lanes of a half may come from any of them).
+template <int ctrl>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, 0xF, 0xF, true));
+}
 template <int D>
-__device__ __forceinline__ u16x8 norm_rotate(u16x8 raw, const uint16_t* w, float eps, int c0,
-                                             int half, const float2* cs) {
-  float x[8];
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xB1>(x);   // quad_perm 1 0 3 2
+  x += dpp<0x4E>(x);   // quad_perm 2 3 0 1
+  x += dpp<0x141>(x);  // row_half_mirror
+  if (D == 128) x += dpp<0x140>(x);  // row_mirror
+  return x;
+}
+
+// What a thread needs for its channels c0 .. c0 + 7 of every row: their norm
+// weights and those of the channels they are turned with.
+template <int D>
+struct Lane {
+  int c0, partner;    // partner: first channel of the other eight
+  bool normed, turned, hi;
+  float w[8], wp[8];
+  __device__ __forceinline__ Lane(const uint16_t* weight, int c0_, int half) : c0(c0_) {
+    turned = c0 < 2 * half;
+    hi = c0 >= half;
+    partner = !turned ? c0 : hi ? c0 - half : c0 + half;
+    normed = weight != nullptr;
+    if (normed) {
+      const u16x8 a = load16(weight + c0), b = load16(weight + partner);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(raw[i]);
-  if (w) {
+      for (int i = 0; i < 8; ++i) {
+        w[i] = bf16_to_f32(a[i]);
+        wp[i] = bf16_to_f32(b[i]);
+      }
+    }
+  }
+};
+
+// A row's eight channels: divided by the row's root mean square and weighted,
+// then rotated with cs (cos, sin of the row's token from the lane's first pair
+// on), in fp32, rounded once to bf16.  All D / 8 lanes of a row take part.
+template <int D>
+__device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, u16x8 other, float eps,
+                                             const float2* cs) {
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = bf16_to_f32(raw[i]);
+    y[i] = bf16_to_f32(other[i]);
+  }
+  if (ln.normed) {
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+    const float inv = __builtin_amdgcn_rsqf(row_sum<D>(ss) * (1.f / D) + eps);
 #pragma unroll
-    for (int s = 1; s < D / 8; s *= 2) ss += __shfl_xor(ss, s);
-    const float inv = 1.f / sqrtf(ss * (1.f / D) + eps);
-    const u16x8 wv = load16(w + c0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * bf16_to_f32(wv[i]);
+    for (int i = 0; i < 8; ++i) {
+      x[i] = x[i] * inv * ln.w[i];
+      y[i] = y[i] * inv * ln.wp[i];
+    }
   }
-  if (half) {
-    const bool hi = c0 >= half;
-    const int partner = static_cast<int>(threadIdx.x & 63) + (hi ? -half : half) / 8;
-    const bool turned = c0 < 2 * half;
-    float y[8];
+  if (ln.turned) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], partner & 63);
-    if (turned) {
-      const float2* t = cs + (hi ? c0 - half : c0);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[i] = hi ? fmaf(x[i], t[i].x, y[i] * t[i].y) : fmaf(x[i], t[i].x, -(y[i] * t[i].y));
+    for (int i = 0; i < 8; ++i) {
+      const float2 t = cs[i];
+      x[i] = fmaf(x[i], t.x, ln.hi ? y[i] * t.y : -(y[i] * t.y));
     }
   }
   u16x8 out;
@@ -91,12 +131,56 @@ __device__ __forceinline__ float2 cos_sin(long pos, double turns) {
 }
 
 template <int D>
-struct StoreShared {
+struct alignas(16) StoreShared {
   union {
     uint32_t nib[kTile * D / 4];       // value codes, a byte each: [token][channel]
-    uint16_t val[kTile][D];            // values: [token][channel]
+    // Values: [token][channel]; rows four elements longer, so that the lanes
+    // that read four groups of eight tokens meet four sets of banks.
+    uint16_t val[kTile][D + 4];
   };
 };
+
+// Queries: p.q_rows consecutive rows (token by token, head by head), the lanes
+// of a row side by side.  The first rows are requested ahead of the angles and
+// the next ones ahead of the arithmetic.
+template <int D>
+__device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item, float2* cs) {
+  constexpr int C8 = D / 8;
+  constexpr int ROWS = kStoreThreads / C8;
+  const unsigned total = static_cast<unsigned>(p.B) * p.T * p.h;
+  const unsigned first = item * p.q_rows, end = min(first + p.q_rows, total);
+  const Lane<D> ln(p.q_w, (threadIdx.x % C8) * 8, p.half);
+  u16x8 raw, other;
+  unsigned r = first + threadIdx.x / C8, tok, head;
+  auto request = [&]() {
+    const unsigned at = min(r, end - 1);  // rows past the end repeat the last one
+    tok = at / static_cast<unsigned>(p.h);
+    head = at - tok * p.h;
+    const uint16_t* row = p.q + tok * p.q_stride + head * D;
+    raw = load16(row + ln.c0);
+    other = ln.turned ? load16(row + ln.partner) : raw;
+  };
+  request();
+  const unsigned tok0 = first / static_cast<unsigned>(p.h);
+  if (p.half) {
+    const unsigned n_tok = (end - 1) / static_cast<unsigned>(p.h) + 1 - tok0;
+    for (unsigned j = threadIdx.x; j < n_tok * p.half; j += kStoreThreads) {
+      const unsigned i = j / p.half, g = tok0 + i, b = g / static_cast<unsigned>(p.T);
+      cs[j] = cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), p.turns[j - i * p.half]);
+    }
+    __syncthreads();
+  }
+  for (unsigned r0 = first; r0 < end; r0 += ROWS) {
+    const u16x8 x = raw, y = other;
+    const unsigned row = r, t = tok, hd = head;
+    r += ROWS;
+    if (r0 + ROWS < end) request();
+    const u16x8 out = norm_rotate<D>(ln, x, y, p.eps,
+                                     cs + (t - tok0) * p.half + (ln.hi ? ln.partner : ln.c0));
+    if (row < end)
+      *reinterpret_cast<u16x8*>(p.q_out + (static_cast<size_t>(t) * p.h + hd) * D + ln.c0) = out;
+  }
+}
 
 template <int D, bool Q4, bool NORM>
 __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
@@ -104,132 +188,121 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   constexpr int ROWS = kStoreThreads / C8;  // token rows a pass of the workgroup takes
   constexpr int PASSES = kTile / ROWS;
   __shared__ StoreShared<D> sm;
-  __shared__ float2 cs[NORM ? kTile * kMaxRopePairs : 1];
+  __shared__ float2 cs[NORM ? kAngleTokens * kMaxRopePairs : 1];
+  const unsigned item = item_of_block();
+  if (item >= p.store_items) {
+    if (NORM && item - p.store_items < p.q_items) norm_queries<D>(p, item - p.store_items, cs);
+    return;
+  }
+  const unsigned unit = item / static_cast<unsigned>(p.tiles);
+  const int tile = static_cast<int>(item - unit * p.tiles);
+  const int b = static_cast<int>(unit / static_cast<unsigned>(p.kv_count));
+  const int c = static_cast<int>(unit - static_cast<unsigned>(b) * p.kv_count);
   const int c8 = threadIdx.x % C8, row = threadIdx.x / C8;
   const int c0 = c8 * 8;
-  for (long item = blockIdx.x; item < p.store_items + (NORM ? p.q_items : 0); item += gridDim.x) {
-    if (NORM && item >= p.store_items) {
-      // Queries: q_tokens tokens of one sequence, all heads.
-      const long i = item - p.store_items;
-      const int per = (p.T + p.q_tokens - 1) / p.q_tokens;
-      const int b = static_cast<int>(i / per), t0 = static_cast<int>(i % per) * p.q_tokens;
-      const int n_tok = min(p.q_tokens, p.T - t0);
-      const long pos0 = (p.starts ? p.starts[b] : 0) + static_cast<long>(t0);
-      for (int j = threadIdx.x; j < n_tok * p.half; j += kStoreThreads) {
-        const int tok = j / p.half, pair = j - tok * p.half;
-        cs[j] = cos_sin(pos0 + tok, p.turns[pair]);
-      }
-      __syncthreads();
-      const int rows = n_tok * p.h;
-      for (int r0 = 0; r0 < rows; r0 += ROWS) {
-        const int r = min(r0 + row, rows - 1);  // rows past the end repeat the last one
-        const int tok = r / p.h, head = r - tok * p.h;
-        const size_t bt = static_cast<size_t>(b) * p.T + t0 + tok;
-        const u16x8 x = load16(p.q + bt * p.q_stride + head * D + c0);
-        const u16x8 y = norm_rotate<D>(x, p.q_w, p.eps, c0, p.half, cs + tok * p.half);
-        if (r0 + row < rows)
-          *reinterpret_cast<u16x8*>(p.q_out + (bt * p.h + head) * D + c0) = y;
-      }
-      __syncthreads();
-      continue;
-    }
-    const int tile = static_cast<int>(item % p.tiles);
-    const long unit = item / p.tiles;
-    const int c = static_cast<int>(unit % p.kv_count), b = static_cast<int>(unit / p.kv_count);
-    const long start = p.starts ? p.starts[b] : 0;
-    const long s0 = ((start >> 5) + tile) * kTile;  // the tile's first slot
-    // Its slots that take a row.
-    const long lo = max(max(start, s0), 0L), end = min(min(start + p.T, s0 + kTile),
-                                                       static_cast<long>(p.S));
-    if (lo >= end) continue;  // uniform over the workgroup
-    const int u_lo = static_cast<int>(lo - s0), u_end = static_cast<int>(end - s0);
-    const size_t seq = static_cast<size_t>(p.kv_begin + c) * p.B + b;
-    uint8_t* const rec =
-        Q4 ? p.q4 + (seq * (p.S / kTile) + s0 / kTile) * QTile<D>::kBytes : nullptr;
-    if (NORM && p.half) {
-      for (int j = threadIdx.x + u_lo * p.half; j < u_end * p.half; j += kStoreThreads) {
-        const int u = j / p.half;
-        cs[j] = cos_sin(s0 + u, p.turns[j - u * p.half]);
-      }
-      __syncthreads();
-    }
+  const long start = p.starts ? p.starts[b] : 0;
+  const long s0 = ((start >> 5) + tile) * kTile;  // the tile's first slot
+  // Its slots that take a row.
+  const long lo = max(max(start, s0), 0L);
+  const long end = min(min(start + p.T, s0 + kTile), static_cast<long>(p.S));
+  if (lo >= end) return;  // uniform over the workgroup
+  const int u_lo = static_cast<int>(lo - s0), u_end = static_cast<int>(end - s0);
+  const size_t seq = static_cast<size_t>(p.kv_begin + c) * p.B + b;
+  uint8_t* const rec = Q4 ? p.q4 + (seq * (p.S / kTile) + s0 / kTile) * QTile<D>::kBytes : nullptr;
+  const Lane<D> ln(NORM ? p.k_w : nullptr, c0, NORM ? p.half : 0);
+  u16x8 xk[PASSES], xv[PASSES], other[PASSES];
 #pragma unroll
-    for (int pass = 0; pass < PASSES; ++pass) {
-      const int u = pass * ROWS + row;
-      const bool live = u >= u_lo && u < u_end;
-      u16x8 xk = {0, 0, 0, 0, 0, 0, 0, 0}, xv = xk;
-      if (live) {
-        const size_t src = static_cast<size_t>(c) * p.s_head + static_cast<size_t>(b) * p.s_seq +
-                           static_cast<size_t>(s0 + u - start) * p.s_tok + c0;
-        xk = load16(p.k_src + src);
-        xv = load16(p.v_src + src);
-      }
-      if (NORM) xk = norm_rotate<D>(xk, p.k_w, p.eps, c0, p.half, cs + u * p.half);
-      if (Q4) {
-        const int ek = block_exp(block_top(xk)), ev = block_exp(block_top(xv));
-        const uint32_t nv = quantise8(xv, ev);
-        // Nibbles 0 .. 3 and 4 .. 7 to bytes.
-        uint32_t lo4 = nv & 0xFFFF, hi4 = nv >> 16;
-        lo4 = (lo4 | lo4 << 8) & 0x00FF00FF;
-        hi4 = (hi4 | hi4 << 8) & 0x00FF00FF;
-        sm.nib[(u * D + c0) / 4] = (lo4 | lo4 << 4) & 0x0F0F0F0F;
-        sm.nib[(u * D + c0) / 4 + 1] = (hi4 | hi4 << 4) & 0x0F0F0F0F;
-        if (live) {
-          *reinterpret_cast<uint32_t*>(rec + QTile<D>::k_dword(u, c8)) = quantise8(xk, ek);
-          if (c8 % 4 == 0) {
-            rec[QTile<D>::k_exp(u, c8 / 4)] = static_cast<uint8_t>(ek);
-            rec[QTile<D>::v_exp(u, c8 / 4)] = static_cast<uint8_t>(ev);
-          }
-        }
-      } else {
-        if (live)
-          *reinterpret_cast<u16x8*>(p.k + (seq * p.S + s0) * D + kchunk<D>(u, c8) * 8) = xk;
-        *reinterpret_cast<u16x8*>(&sm.val[u][c0]) = xv;
-      }
+  for (int pass = 0; pass < PASSES; ++pass) {
+    const int u = pass * ROWS + row;
+    const u16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+    xk[pass] = xv[pass] = other[pass] = zero;
+    if (u >= u_lo && u < u_end) {
+      const size_t src = static_cast<size_t>(c) * p.s_head + static_cast<size_t>(b) * p.s_seq +
+                         static_cast<size_t>(s0 + u - start) * p.s_tok;
+      xk[pass] = load16(p.k_src + src + c0);
+      xv[pass] = load16(p.v_src + src + c0);
+      if (NORM && ln.turned) other[pass] = load16(p.k_src + src + ln.partner);
+    }
+  }
+  if (NORM && p.half) {
+    for (int j = threadIdx.x + u_lo * p.half; j < u_end * p.half; j += kStoreThreads) {
+      const int u = j / p.half;
+      cs[j] = cos_sin(s0 + u, p.turns[j - u * p.half]);
     }
     __syncthreads();
-    // Values, eight tokens of a channel at a time; tokens without a new row
-    // keep what the slot holds.
-    for (int i = threadIdx.x; i < 4 * D; i += kStoreThreads) {
-      int d, g;
-      if (Q4) {  // in the order of the record's dwords
-        const int lane = (i >> 2) & 63;
-        d = ((i >> 8) * 4 + (i & 3)) * 16 + (lane & 15);
-        g = lane >> 4;
-      } else {
-        d = i >> 2;
-        g = i & 3;
+  }
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    const int u = pass * ROWS + row;
+    const bool live = u >= u_lo && u < u_end;
+    u16x8 k = xk[pass];
+    const u16x8 v = xv[pass];
+    if (NORM)
+      k = norm_rotate<D>(ln, k, other[pass], p.eps, cs + u * p.half + (ln.hi ? ln.partner : c0));
+    if (Q4) {
+      const int ek = block_exp(block_top(k)), ev = block_exp(block_top(v));
+      const uint32_t nv = quantise8(v, ev);
+      // Nibbles 0 .. 3 and 4 .. 7 to bytes.
+      uint32_t lo4 = nv & 0xFFFF, hi4 = nv >> 16;
+      lo4 = (lo4 | lo4 << 8) & 0x00FF00FF;
+      hi4 = (hi4 | hi4 << 8) & 0x00FF00FF;
+      sm.nib[(u * D + c0) / 4] = (lo4 | lo4 << 4) & 0x0F0F0F0F;
+      sm.nib[(u * D + c0) / 4 + 1] = (hi4 | hi4 << 4) & 0x0F0F0F0F;
+      if (live) {
+        *reinterpret_cast<uint32_t*>(rec + QTile<D>::k_dword(u, c8)) = quantise8(k, ek);
+        if (c8 % 4 == 0) {
+          rec[QTile<D>::k_exp(u, c8 / 4)] = static_cast<uint8_t>(ek);
+          rec[QTile<D>::v_exp(u, c8 / 4)] = static_cast<uint8_t>(ev);
+        }
       }
-      const int first = max(u_lo - 8 * g, 0), last = min(u_end - 8 * g, 8);
-      if (first >= last) continue;
-      if (Q4) {
-        uint32_t* dst = reinterpret_cast<uint32_t*>(rec + QTile<D>::kVCodes) + i;
-        uint32_t w = 0;
+    } else {
+      if (live) *reinterpret_cast<u16x8*>(p.k + (seq * p.S + s0) * D + kchunk<D>(u, c8) * 8) = k;
+      const uint4 d = __builtin_bit_cast(uint4, v);
+      *reinterpret_cast<uint2*>(&sm.val[u][c0]) = make_uint2(d.x, d.y);
+      *reinterpret_cast<uint2*>(&sm.val[u][c0 + 4]) = make_uint2(d.z, d.w);
+    }
+  }
+  __syncthreads();
+  // Values, eight tokens of a channel at a time; tokens without a new row keep
+  // what the slot holds.
+  for (int i = threadIdx.x; i < 4 * D; i += kStoreThreads) {
+    int d, g;
+    if (Q4) {  // in the order of the record's dwords
+      const int lane = (i >> 2) & 63;
+      d = ((i >> 8) * 4 + (i & 3)) * 16 + (lane & 15);
+      g = lane >> 4;
+    } else {
+      d = i >> 2;
+      g = i & 3;
+    }
+    const int first = max(u_lo - 8 * g, 0), last = min(u_end - 8 * g, 8);
+    if (first >= last) continue;
+    if (Q4) {
+      uint32_t* dst = reinterpret_cast<uint32_t*>(rec + QTile<D>::kVCodes) + i;
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        w |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(sm.nib)[(8 * g + e) * D + d])
+             << (4 * e);
+      if (last - first < 8) {
+        const uint32_t taken =
+            (last == 8 ? ~0u : (1u << (4 * last)) - 1) & ~((1u << (4 * first)) - 1);
+        w = (w & taken) | (*dst & ~taken);
+      }
+      *dst = w;
+    } else {
+      uint16_t* dst = p.v + (seq * p.S + s0) * D + d * kTile + 8 * g;
+      u16x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = sm.val[8 * g + e][d];
+      if (last - first == 8) {
+        *reinterpret_cast<u16x8*>(dst) = w;
+      } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          w |= static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(sm.nib)[(8 * g + e) * D + d])
-               << (4 * e);
-        if (last - first < 8) {
-          const uint32_t taken =
-              (last == 8 ? ~0u : (1u << (4 * last)) - 1) & ~((1u << (4 * first)) - 1);
-          w = (w & taken) | (*dst & ~taken);
-        }
-        *dst = w;
-      } else {
-        uint16_t* dst = p.v + (seq * p.S + s0) * D + d * kTile + 8 * g;
-        u16x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = sm.val[8 * g + e][d];
-        if (last - first == 8) {
-          *reinterpret_cast<u16x8*>(dst) = w;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e >= first && e < last) dst[e] = w[e];
-        }
+          if (e >= first && e < last) dst[e] = w[e];
       }
     }
-    __syncthreads();  // the next item reuses the LDS
   }
 }
 
@@ -239,53 +312,49 @@ __global__ __launch_bounds__(kStoreThreads) void read_kernel(ReadParams p) {
   constexpr int ROWS = kStoreThreads / C8;
   __shared__ uint32_t codes[4 * D];  // the tile's value codes
   const int c8 = threadIdx.x % C8, row = threadIdx.x / C8;
-  for (long item = blockIdx.x; item < p.items; item += gridDim.x) {
-    const int tile = static_cast<int>(item % p.tiles);
-    const long unit = item / p.tiles;
-    const int b = static_cast<int>(unit % p.B), c = static_cast<int>(unit / p.B);
-    const long start = p.starts ? p.starts[b] : 0;
-    const long s0 = ((start >> 5) + tile) * kTile;
-    const long lo = max(start, s0), end = min(start + p.T, s0 + kTile);
-    if (lo >= end) continue;
-    const bool held = s0 >= 0 && s0 < p.S;  // other slots read as zeros
-    const size_t seq = static_cast<size_t>(p.kv_begin + c) * p.B + b;
-    const uint8_t* rec = p.q4 + (seq * (p.S / kTile) + (held ? s0 / kTile : 0)) * QTile<D>::kBytes;
-    if (held)
-      for (int i = threadIdx.x; i < 4 * D; i += kStoreThreads)
-        codes[i] = reinterpret_cast<const uint32_t*>(rec + QTile<D>::kVCodes)[i];
-    __syncthreads();
-    for (int u = row; u < kTile; u += ROWS) {
-      if (s0 + u < lo || s0 + u >= end) continue;
-      u16x8 xk = {0, 0, 0, 0, 0, 0, 0, 0}, xv = xk;
-      if (held) {
-        xk = dequantise8(*reinterpret_cast<const uint32_t*>(rec + QTile<D>::k_dword(u, c8)),
-                         exp_scale(rec[QTile<D>::k_exp(u, c8 / 4)]));
-        uint32_t w = 0;
+  const unsigned item = item_of_block();
+  if (item >= p.items) return;
+  const unsigned unit = item / static_cast<unsigned>(p.tiles);
+  const int tile = static_cast<int>(item - unit * p.tiles);
+  const int c = static_cast<int>(unit / static_cast<unsigned>(p.B));
+  const int b = static_cast<int>(unit - static_cast<unsigned>(c) * p.B);
+  const long start = p.starts ? p.starts[b] : 0;
+  const long s0 = ((start >> 5) + tile) * kTile;
+  const long lo = max(start, s0), end = min(start + p.T, s0 + kTile);
+  if (lo >= end) return;
+  const bool held = s0 >= 0 && s0 < p.S;  // other slots read as zeros
+  const size_t seq = static_cast<size_t>(p.kv_begin + c) * p.B + b;
+  const uint8_t* rec = p.q4 + (seq * (p.S / kTile) + (held ? s0 / kTile : 0)) * QTile<D>::kBytes;
+  if (held)
+    for (int i = threadIdx.x; i < 4 * D; i += kStoreThreads)
+      codes[i] = reinterpret_cast<const uint32_t*>(rec + QTile<D>::kVCodes)[i];
+  __syncthreads();
+  for (int u = row; u < kTile; u += ROWS) {
+    if (s0 + u < lo || s0 + u >= end) continue;
+    u16x8 xk = {0, 0, 0, 0, 0, 0, 0, 0}, xv = xk;
+    if (held) {
+      xk = dequantise8(*reinterpret_cast<const uint32_t*>(rec + QTile<D>::k_dword(u, c8)),
+                       exp_scale(rec[QTile<D>::k_exp(u, c8 / 4)]));
+      uint32_t w = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = c8 * 8 + e, db = d >> 4;
-          const int at = (db >> 2) * 256 + ((u >> 3) * 16 + (d & 15)) * 4 + (db & 3);
-          w |= ((codes[at] >> (4 * (u & 7))) & 15) << (4 * e);
-        }
-        xv = dequantise8(w, exp_scale(rec[QTile<D>::v_exp(u, c8 / 4)]));
+      for (int e = 0; e < 8; ++e) {
+        const int d = c8 * 8 + e, db = d >> 4;
+        const int at = (db >> 2) * 256 + ((u >> 3) * 16 + (d & 15)) * 4 + (db & 3);
+        w |= ((codes[at] >> (4 * (u & 7))) & 15) << (4 * e);
       }
-      const size_t dst = ((static_cast<size_t>(c) * p.B + b) * p.T +
-                          static_cast<size_t>(s0 + u - start)) * D + c8 * 8;
-      *reinterpret_cast<u16x8*>(p.k_rows + dst) = xk;
-      *reinterpret_cast<u16x8*>(p.v_rows + dst) = xv;
+      xv = dequantise8(w, exp_scale(rec[QTile<D>::v_exp(u, c8 / 4)]));
     }
-    __syncthreads();
+    const size_t dst = ((static_cast<size_t>(c) * p.B + b) * p.T +
+                        static_cast<size_t>(s0 + u - start)) * D + c8 * 8;
+    *reinterpret_cast<u16x8*>(p.k_rows + dst) = xk;
+    *reinterpret_cast<u16x8*>(p.v_rows + dst) = xv;
   }
-}
-
-dim3 store_grid(long items) {
-  return dim3(static_cast<unsigned>(items < kMaxStoreGrid ? items : kMaxStoreGrid));
 }
 
 }  // namespace
 
 hipError_t launch_store(const StoreParams& p, int head_dim, bool norm, hipStream_t stream) {
-  const dim3 grid = store_grid(p.store_items + (norm ? p.q_items : 0));
+  const dim3 grid = item_grid(p.store_items + (norm ? p.q_items : 0));
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kStoreThreads), 0, stream, p);
     return hipGetLastError();
@@ -300,7 +369,7 @@ hipError_t launch_store(const StoreParams& p, int head_dim, bool norm, hipStream
 
 hipError_t launch_qcache_read(const ReadParams& p, int head_dim, hipStream_t stream) {
   auto kernel = head_dim == 64 ? read_kernel<64> : read_kernel<128>;
-  hipLaunchKernelGGL(kernel, store_grid(p.items), dim3(kStoreThreads), 0, stream, p);
+  hipLaunchKernelGGL(kernel, item_grid(p.items), dim3(kStoreThreads), 0, stream, p);
   return hipGetLastError();
 }
 

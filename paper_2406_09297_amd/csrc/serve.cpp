@@ -72,9 +72,14 @@ int touched_tiles(int T, bool from_zero) {
   return static_cast<int>((T + first + kTileTokens - 1) / kTileTokens);
 }
 
-mlkv::StoreParams store_params(const mlkv_qcache* q4, const mlkv_cache* bf16, int T, int kv_begin,
-                               int kv_count, const int32_t* starts) {
-  mlkv::StoreParams p{};
+mlkv_status check_blocks(int kv_count, int batch, int tiles) {
+  if (static_cast<double>(kv_count) * batch * tiles > 2147483647.0)
+    return fail(MLKV_ERR_CAPACITY, "more than 2^31 - 1 blocks of 32 tokens in one call");
+  return MLKV_OK;
+}
+
+mlkv_status store_params(const mlkv_qcache* q4, const mlkv_cache* bf16, int T, int kv_begin,
+                         int kv_count, const int32_t* starts, mlkv::StoreParams& p) {
   if (q4) {
     p.q4 = static_cast<uint8_t*>(q4->data);
     p.B = q4->batch;
@@ -90,8 +95,9 @@ mlkv::StoreParams store_params(const mlkv_qcache* q4, const mlkv_cache* bf16, in
   p.kv_count = kv_count;
   p.starts = starts;
   p.tiles = touched_tiles(T, !starts);
-  p.store_items = static_cast<long>(kv_count) * p.B * p.tiles;
-  return p;
+  const mlkv_status s = check_blocks(kv_count, p.B, p.tiles);
+  if (s == MLKV_OK) p.store_items = static_cast<unsigned>(kv_count) * p.B * p.tiles;
+  return s;
 }
 
 mlkv_status launch_store_checked(const mlkv::StoreParams& p, int head_dim, bool norm,
@@ -241,6 +247,8 @@ mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, con
   return ok();
 }
 
+constexpr long kQueryGroupsPerCu = 8, kMaxQueryPasses = 4;
+
 mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* bf16,
                              const mlkv_qcache* q4, const void* q, int q_row_stride,
                              const void* k_new, const void* v_new, int new_row_stride, int T,
@@ -271,8 +279,10 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
                 q_row_stride, static_cast<long>(h) * D);
   if (owned > 0 && (s = check_new_rows(k_new, v_new, new_row_stride, owned, D)) != MLKV_OK) return s;
   if ((s = check_prefill_lengths_if_requested(ctx_lens, B, T, S, stream)) != MLKV_OK) return s;
-  mlkv::StoreParams p =
-      store_params(q4, bf16, T, owned > 0 ? map->own_begin[layer] : 0, owned, ctx_lens);
+  mlkv::StoreParams p{};
+  if ((s = store_params(q4, bf16, T, owned > 0 ? map->own_begin[layer] : 0, owned, ctx_lens, p)) !=
+      MLKV_OK)
+    return s;
   p.k_src = static_cast<const uint16_t*>(k_new);
   p.v_src = static_cast<const uint16_t*>(v_new);
   p.s_head = D;
@@ -284,13 +294,32 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
   p.q_out = static_cast<uint16_t*>(q_out);
   p.q_stride = q_row_stride;
   p.h = h;
-  // Eight tokens share the sines of a query workgroup.
-  p.q_tokens = T < 8 ? T : 8;
-  p.q_items = static_cast<long>(B) * ((T + p.q_tokens - 1) / p.q_tokens);
+  // A query workgroup takes its rows in passes, more where there are workgroups
+  // enough for every compute unit, of at most kAngleTokens tokens.
+  const double rows = static_cast<double>(B) * T * h;
+  if (rows > 2147483647.0)
+    return fail(MLKV_ERR_UNSUPPORTED, "%.0f query rows: at most 2^31 - 1", rows);
+  const long per_pass = mlkv::kStoreThreads / (D / 8), total = static_cast<long>(rows);
+  const long most = (static_cast<long>(mlkv::kAngleTokens - 2) * h + 1) / per_pass;
+  long passes = total / (per_pass * kQueryGroupsPerCu * compute_units_or_fallback());
+  passes = passes < most ? passes : most;
+  passes = passes < 1 ? 1 : passes > kMaxQueryPasses ? kMaxQueryPasses : passes;
+  p.q_rows = static_cast<unsigned>(per_pass * passes);
+  p.q_items = static_cast<unsigned>((total + p.q_rows - 1) / p.q_rows);
+  if (static_cast<double>(p.store_items) + p.q_items > 2147483647.0)
+    return fail(MLKV_ERR_CAPACITY, "more than 2^31 - 1 workgroups in one call");
   p.half = nr->rotary_dims / 2;
   p.eps = static_cast<float>(nr->eps);
-  for (int j = 0; j < p.half; ++j)
-    p.turns[j] = std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims) * 0.15915494309189533577;
+  // Revolutions base^(-2j / dims) / 2 pi, as the product of two powers each
+  // (sixteen powers instead of up to 64, 3 us of a call).
+  double fine[8];
+  for (int j = 0; j < 8 && j < p.half; ++j)
+    fine[j] = std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims);
+  for (int j = 0; j < p.half; j += 8) {
+    const double coarse =
+        std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims) * 0.15915494309189533577;
+    for (int i = 0; i < 8; ++i) p.turns[j + i] = coarse * fine[i];
+  }
   return launch_store_checked(p, D, true, stream);
 }
 
@@ -323,7 +352,9 @@ mlkv_status mlkv_qcache_append_rows(int layer, const mlkv_map* map, const mlkv_q
   if ((s = check_prefill_lengths_if_requested(ctx_lens, cache->batch, T, cache->capacity,
                                               stream)) != MLKV_OK)
     return s;
-  mlkv::StoreParams p = store_params(cache, nullptr, T, map->own_begin[layer], owned, ctx_lens);
+  mlkv::StoreParams p{};
+  if ((s = store_params(cache, nullptr, T, map->own_begin[layer], owned, ctx_lens, p)) != MLKV_OK)
+    return s;
   p.k_src = static_cast<const uint16_t*>(k_new);
   p.v_src = static_cast<const uint16_t*>(v_new);
   p.s_head = cache->head_dim;
@@ -339,7 +370,8 @@ mlkv_status mlkv_qcache_write_rows(const mlkv_qcache* cache, int kv_begin, int k
   if ((s = check_rows(cache, kv_begin, kv_count, starts, T)) != MLKV_OK) return s;
   if (kv_count == 0 || T == 0) return ok();
   if ((s = check_row_buffers(k_rows, v_rows)) != MLKV_OK) return s;
-  mlkv::StoreParams p = store_params(cache, nullptr, T, kv_begin, kv_count, starts);
+  mlkv::StoreParams p{};
+  if ((s = store_params(cache, nullptr, T, kv_begin, kv_count, starts, p)) != MLKV_OK) return s;
   p.k_src = static_cast<const uint16_t*>(k_rows);
   p.v_src = static_cast<const uint16_t*>(v_rows);
   p.s_tok = cache->head_dim;
@@ -366,7 +398,8 @@ mlkv_status mlkv_qcache_read_rows(const mlkv_qcache* cache, int kv_begin, int kv
   p.kv_begin = kv_begin;
   p.kv_count = kv_count;
   p.tiles = touched_tiles(T, !starts);
-  p.items = static_cast<long>(kv_count) * p.B * p.tiles;
+  if ((s = check_blocks(kv_count, p.B, p.tiles)) != MLKV_OK) return s;
+  p.items = static_cast<unsigned>(kv_count) * p.B * p.tiles;
   const hipError_t err = mlkv::launch_qcache_read(p, cache->head_dim, stream);
   if (err != hipSuccess) return fail(MLKV_ERR_HIP, "cache rows launch: %s", hipGetErrorString(err));
   return ok();

@@ -36,15 +36,15 @@ struct StoreParams {
   uint8_t* q4;                // 4-bit cache, or null:
   uint16_t *k, *v;            // bf16 planes
   int B, T, S, kv_begin, kv_count;
-  long store_items;           // kv_count * B * tiles a sequence's rows may touch
+  unsigned store_items;       // kv_count * B * tiles a sequence's rows may touch
   int tiles;
   // Norm and rotation of keys and queries (norm kernels only).
   const uint16_t *q_w, *k_w;  // [D] norm weights, or null: no norm
   const uint16_t* q;          // row (b, t) at q + (b*T + t)*q_stride: [h][D]
   uint16_t* q_out;            // [B][T][h][D]
   size_t q_stride;
-  int h, q_tokens;            // tokens of a query workgroup
-  long q_items;               // query workgroups
+  int h;
+  unsigned q_rows, q_items;   // (token, head) rows of a query workgroup, and these workgroups
   int half;                   // rotated channel pairs (0: none)
   float eps;
   double turns[kMaxRopePairs];  // revolutions a position turns pair j by
@@ -55,9 +55,11 @@ struct ReadParams {
   uint16_t *k_rows, *v_rows;  // [kv_count][B][T][D]
   const int32_t* starts;      // row t of sequence b is slot starts[b] + t (null: t)
   int B, T, S, kv_begin, kv_count, tiles;
-  long items;
+  unsigned items;
 };
 
+constexpr int kStoreThreads = 256;
+constexpr int kAngleTokens = 33;  // whose sines a workgroup holds
 hipError_t launch_store(const StoreParams& p, int head_dim, bool norm, hipStream_t stream);
 hipError_t launch_qcache_read(const ReadParams& p, int head_dim, hipStream_t stream);
 

@@ -317,7 +317,10 @@ void span_kernel(SpanParams p) {
   // Row rr, channels d .. d + 3 of partial `slot`, or of the output (slot -1).
   auto put = [&](int slot, int rr, int d, f32x4 o, float m, float den) {
     if (slot < 0) {
-      store4_as<D>(p.out, p.out_bf16, out_row + rr, d, normalize4(o, den));
+      // A row that attends nothing is zero; one whose scores are all -inf has a
+      // denominator of zero too, and is NaN.
+      const f32x4 y = sp.L > 0 ? o * __builtin_amdgcn_rcpf(den) : f32x4{0.f, 0.f, 0.f, 0.f};
+      store4_as<D>(p.out, p.out_bf16, out_row + rr, d, y);
       return;
     }
     store4_device(rsrc, (slot * part_floats + rr * D + d) * 4, o);

@@ -210,6 +210,81 @@ def test_decode_captured_in_a_graph_follows_the_lengths(four_bits):
         assert torch.equal(out, c.decode())
 
 
+@pytest.mark.parametrize("L", [40, 700])
+def test_scores_that_are_all_minus_infinity_give_nan(L):
+    """The quotient is 0 / 0; a sequence with one finite score has its value."""
+    c = Case(False, 4, 1, 64, [L, L, 0], 704, 58)
+    k, v = (t.clone() for t in c.cache.read_rows(1, 1))
+    c.q[:, :, 0] = 1.0
+    k[0, :, :L, 0] = -float("inf")
+    k[0, 1, L - 7, 0] = 1.0
+    c.cache.write_rows(k, v, 1)
+    out = c.decode()
+    assert out[0].isnan().all() and not out[2].any()
+    assert torch.equal(out[1], v[0, 1, L - 7].float().expand(4, 64))
+    pre = torch.empty((3, 1, 4, 64), dtype=torch.float32, device="cuda")
+    c.seq_lens[2] = 1  # prefill has a token in every sequence
+    mlkv.prefill_attention_window(3, c.q.view(3, 1, 4, 64), c.cache, c.map, c.seq_lens - 1, pre, 0)
+    assert pre[0].isnan().all()
+    assert torch.equal(pre[1, 0], v[0, 1, L - 7].float().expand(4, 64))
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_caches_beyond_32_bit_offsets(four_bits):
+    """The last head and sequence of a cache of more than 2^32 bytes (4-bit) or
+    elements a plane (bf16), near the end of a long capacity."""
+    D, S, g, B = 128, 1 << 20, 17, 2
+    label = f"large {'4-bit' if four_bits else 'bf16'}"
+    say(label)
+    mp = mlkv.Map.uniform(4, 2 * g, 2, g)
+    cache = (mlkv.QCache if four_bits else mlkv.Cache).empty(2 * g, B, S, D)
+    n, window, L = 100, 60, S - 3
+    shape = (B, n, g, D)
+    k, v = synth.normal_bf16(59, 1, shape), synth.normal_bf16(59, 2, shape)
+    kd, vd = mlkv.bf16_tensor(k, "cuda"), mlkv.bf16_tensor(v, "cuda")
+    ctx = torch.full((B,), L - n, dtype=torch.int32, device="cuda")
+    if four_bits:
+        mlkv.qcache_append_rows(2, mp, cache, kd, vd, ctx)
+        back = cache.read_rows(2 * g - 1, 1, starts=ctx, T=n)
+        k, v = serve_ref.held(k), serve_ref.held(v)
+        for got, want in zip(back, (k, v)):
+            assert np.array_equal(got[0].double().cpu().numpy(), want[:, :, g - 1])
+    else:
+        mlkv.cache_append_rows(2, mp, cache, kd, vd, ctx, n)
+        k, v = serve_ref.f64(k), serve_ref.f64(v)
+    q_bits = synth.normal_bf16(59, 3, (B, 2 * g, D))
+    q = mlkv.bf16_tensor(q_bits, "cuda")
+    out = torch.empty((B, 2 * g, D), dtype=torch.float32, device="cuda")
+    ws = mlkv.window_workspace(mp, B, S, D)
+    f = mlkv.qcache_decode_attention if four_bits else mlkv.decode_attention_window
+    f(3, q, cache, mp, ctx + n, out, window=window, ws=ws)
+    outs = [out]
+    if not four_bits:
+        pre = torch.empty((B, 1, 2 * g, D), dtype=torch.float32, device="cuda")
+        mlkv.prefill_attention_window(3, q[:, None].contiguous(), cache, mp, ctx + (n - 1), pre,
+                                      window)
+        outs.append(pre[:, 0])
+    for o in outs:
+        o = o.double().cpu().numpy()
+        for b in range(B):
+            for r in (0, g - 1):
+                hs = slice(2 * r, 2 * r + 2)
+                ref, bound = serve_ref.attend(serve_ref.f64(q_bits[b, hs]), k[b, :, r], v[b, :, r],
+                                              np.arange(n - window, n))
+                assert np.all(np.abs(o[b, hs] - ref) <= bound), (label, b, r)
+
+
+def test_lengths_are_checked_on_request(monkeypatch):
+    c = Case(True, 4, 1, 64, [64, 40], 64, 60)
+    monkeypatch.setenv("MLKV_CHECK", "1")
+    c.decode()
+    with pytest.raises(mlkv.MLKVError, match="attends 64 positions, limit 50"):
+        c.decode(hint=50)
+    rows = torch.zeros((2, 3, 1, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(mlkv.MLKVError, match="64 cached"):
+        mlkv.qcache_append_rows(2, c.map, c.cache, rows, rows, c.seq_lens)
+
+
 # ------------------------------------------------------------------ prefill ---
 
 @pytest.mark.parametrize("D,h,g", [(64, 12, 1), (128, 8, 2)])
