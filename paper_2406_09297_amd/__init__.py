@@ -287,6 +287,7 @@ class Cache:
         self.n_kv, self.batch, self.capacity, self.head_dim = n_kv, B, S, D
         self._c = _Cache(_dev_ptr(k, torch.bfloat16, "cache.k"),
                          _dev_ptr(v, torch.bfloat16, "cache.v"), n_kv, B, S, D)
+        self._device = k.get_device()
 
     @classmethod
     def empty(cls, n_kv: int, batch: int, capacity: int, head_dim: int, device="cuda") -> "Cache":
@@ -493,8 +494,8 @@ def _rows_arg(t: torch.Tensor, shape, device: int, name: str):
 
 def _launch_device(device: int) -> int:
     """The cache's device, which must be the current one: kernels are launched there."""
-    if device != torch.cuda.current_device():
-        raise ValueError(f"tensors on cuda:{device}, current device {torch.cuda.current_device()}")
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on device {device}, which is not the current one")
     return device
 
 
@@ -503,7 +504,7 @@ def _ws_args(ws, device: int):
         return None, 0
     if ws.get_device() != device or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous tensor on cuda:{device}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 class QCache:
@@ -520,6 +521,7 @@ class QCache:
             raise ValueError("data must be [n_kv][B][S/32][34 D] with D 64 or 128")
         self._c = _QCache(_dev_ptr(data, torch.uint8, "data"), n_kv, B, self.capacity,
                           self.head_dim)
+        self._device = data.get_device()
 
     @classmethod
     def empty(cls, n_kv: int, batch: int, capacity: int, head_dim: int, device="cuda") -> "QCache":
@@ -534,7 +536,7 @@ class QCache:
 
     def _rows(self, starts, n: int, T: int):
         """(device, starts pointer, row shape) of a conversion."""
-        device = _launch_device(self.data.get_device())
+        device = _launch_device(self._device)
         at = None if starts is None else _arg(starts, (self.batch,), torch.int32, device, "starts")
         return device, at, (n, self.batch, T, self.head_dim)
 
@@ -563,12 +565,6 @@ class QCache:
         return k, v
 
 
-def _cache_of(cache):
-    """The ctypes structure and the device of a Cache or QCache."""
-    return cache.struct, _launch_device(cache.data.get_device() if isinstance(cache, QCache)
-                                        else cache.k.get_device())
-
-
 def _new_rows(layer: int, map_: Map, cache, k_new, v_new, T: int, device: int):
     """Pointers and row stride of a layer's T new keys and values."""
     shape = (cache.batch, T, map_._owned[layer], cache.head_dim)
@@ -589,10 +585,10 @@ def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor
     """mlkv_qcache_append_rows: k_new/v_new [B][T][owned][D] (rows may be columns
     of a wider tensor's), stored at slots ctx_lens[b] + t."""
     _check_layer(layer, map_)
-    struct, device = _cache_of(cache)
+    device = _launch_device(cache._device)
     k, v, stride = _new_rows(layer, map_, cache, k_new, v_new, k_new.shape[1], device)
     _check(lib().mlkv_qcache_append_rows(
-        layer, map_.handle, struct, k, v, k_new.shape[1], stride,
+        layer, map_.handle, cache.struct, k, v, k_new.shape[1], stride,
         _arg(ctx_lens, (cache.batch,), torch.int32, device, "ctx_lens"), _stream(stream)))
 
 
@@ -607,12 +603,13 @@ def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device
 
 def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, max_len_hint, ws,
                       stream):
-    struct, device = _cache_of(cache)
+    device = _launch_device(cache._device)
     shape = (cache.batch, map_._heads, cache.head_dim)
-    _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), struct, map_.handle,
-             _arg(seq_lens, shape[:1], torch.int32, device, "seq_lens"), window, sinks,
-             _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint,
-             *_ws_args(ws, device), _stream(stream)))
+    ws_ptr, ws_bytes = _ws_args(ws, device)
+    _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_._h,
+             _arg(seq_lens, (shape[0],), torch.int32, device, "seq_lens"), window, sinks,
+             _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint, ws_ptr,
+             ws_bytes, _stream(stream)))
 
 
 def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Map,
@@ -640,10 +637,10 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
                              sinks: int = 0, stream=None):
     """mlkv_prefill_attention_window: q [B][T][h][D] bf16 -> out [B][T][h][D]
     (fp32 or bf16); token t of sequence b stands at position ctx_lens[b] + t."""
-    struct, device = _cache_of(cache)
+    device = _launch_device(cache._device)
     shape = (cache.batch, q.shape[1], map_._heads, cache.head_dim)
     _check(lib().mlkv_prefill_attention_window(
-        layer, _arg(q, shape, torch.bfloat16, device, "q"), struct, map_.handle,
+        layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_.handle,
         _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
         _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _stream(stream)))
 
@@ -660,7 +657,7 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
     None where the layer owns no head).  q, k_new and v_new may be columns of
     one projection's rows."""
     _check_layer(layer, map_)
-    struct, device = _cache_of(cache)
+    device = _launch_device(cache._device)
     B, T, h, D = cache.batch, q.shape[1], map_._heads, cache.head_dim
     qp, q_stride = _rows_arg(q, (B, T, h, D), device, "q")
     kp = vp = None
@@ -675,7 +672,7 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
         eps, rotary_dims, rotary_base)
     L = lib()
     f = L.mlkv_qcache_norm_rope_append if isinstance(cache, QCache) else L.mlkv_norm_rope_append
-    _check(f(layer, map_.handle, struct, qp, q_stride, kp, vp, stride, T,
+    _check(f(layer, map_.handle, cache.struct, qp, q_stride, kp, vp, stride, T,
              _arg(ctx_lens, (B,), torch.int32, device, "ctx_lens"), ctypes.byref(nr),
              _arg(q_out, (B, T, h, D), torch.bfloat16, device, "q_out"), _stream(stream)))
 
