@@ -210,3 +210,98 @@ def test_a_layer_of_a_serving_loop(D, h, g, window, sinks):
             mlkv.qcache_decode_attention(layer, q1, four, mp, ctx + 1, o1, window, sinks, ws=ws)
             check(out, q_bf16, cached4, n0, 1, f"step {step} layer {layer} 4-bit")
         ctx = ctx + n
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_a_decode_step_captured_in_a_graph(four_bits):
+    """Norm, rotation, append and attention of a layer as one graph: each replay
+    follows the new projections and lengths, as the eager calls do on a cache of
+    their own; split runs, several replays, eager work in between."""
+    D, h, g, B, S, window = 64, 12, 4, 2, 1024, 500
+    mp = mlkv.Map.uniform(2, h, 1, g)
+    kind = mlkv.QCache if four_bits else mlkv.Cache
+    caches = [kind.empty(g, B, S, D) for _ in range(2)]
+    k, v = (mlkv.bf16_tensor(synth.normal_bf16(90, s, (g, B, S, D)), "cuda") for s in (1, 2))
+    for cache in caches:
+        cache.write_rows(k, v)
+    w = mlkv.bf16_tensor(_weight(8, D), "cuda")
+    x = torch.empty((B, 1, (h + 2 * g) * D), dtype=torch.bfloat16, device="cuda")
+    ctx = torch.tensor([900, 30], dtype=torch.int32, device="cuda")
+    lens = ctx + 1
+    workspaces = [mlkv.window_workspace(mp, B, S, D) for _ in range(2)]
+    attend = mlkv.qcache_decode_attention if four_bits else mlkv.decode_attention_window
+
+    def step(cache, ws, q_out, out):
+        q, kn, vn = (x[..., a * D:(a + n) * D].unflatten(-1, (n, D))
+                     for a, n in ((0, h), (h, g), (h + g, g)))
+        mlkv.norm_rope_append(0, mp, cache, q, kn, vn, ctx, q_out, q_norm=w, k_norm=w,
+                              rotary_dims=D)
+        attend(0, q_out.view(B, h, D), cache, mp, lens, out, window=window, sinks=4, ws=ws)
+
+    outs = [torch.empty((B, h, D), dtype=torch.float32, device="cuda") for _ in range(2)]
+    qs = [torch.empty((B, 1, h, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    x.normal_()
+    step(caches[0], workspaces[0], qs[0], outs[0])
+    step(caches[1], workspaces[1], qs[1], outs[1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(caches[0], workspaces[0], qs[0], outs[0])
+    for n in range(4):
+        x.copy_(mlkv.bf16_tensor(synth.normal_bf16(91 + n, 0, tuple(x.shape)), "cuda"))
+        ctx.add_(1)
+        lens.add_(1)
+        graph.replay()
+        step(caches[1], workspaces[1], qs[1], outs[1])
+        torch.cuda.synchronize()
+        assert torch.equal(qs[0], qs[1]) and torch.equal(outs[0], outs[1]), n
+        pairs = [(caches[0].data, caches[1].data)] if four_bits else \
+            [(caches[0].k, caches[1].k), (caches[0].v, caches[1].v)]
+        for a, b in pairs:
+            assert torch.equal(a, b)
+
+
+def test_prompt_calls_on_a_stream_of_their_own_and_in_a_graph():
+    """Append, norm and windowed prefill of a prompt: on another stream and
+    replayed from a graph, the same results."""
+    D, h, g, B, T, S = 128, 8, 2, 2, 70, 128
+    mp = mlkv.Map.uniform(2, h, 1, g)
+    _, (q, k, v) = _projected(95, B, T, h, g, D)
+    ctx = torch.tensor([3, 40], dtype=torch.int32, device="cuda")
+    old = [mlkv.bf16_tensor(synth.normal_bf16(96, s, (g, B, S, D)), "cuda") for s in (1, 2)]
+
+    def run(stream=None):
+        bf16, four = mlkv.Cache.empty(g, B, S, D), mlkv.QCache.empty(g, B, S, D)
+        bf16.write_rows(*old, stream=stream)
+        four.write_rows(*old, stream=stream)
+        q_out = torch.empty((B, T, h, D), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty((B, T, h, D), dtype=torch.bfloat16, device="cuda")
+
+        def calls():
+            mlkv.norm_rope_append(0, mp, bf16, q, k, v, ctx, q_out, rotary_dims=32, stream=stream)
+            mlkv.prefill_attention_window(0, q_out, bf16, mp, ctx, out, 33, 2, stream=stream)
+            mlkv.qcache_append_rows(0, mp, four, k, v, ctx, stream=stream)
+        return calls, (bf16.k, bf16.v, four.data, q_out, out)
+
+    calls, want = run()
+    calls()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    calls, got = run(side)
+    calls()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    calls, got = run()
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(3):
+        got[3].zero_()
+        got[4].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

@@ -348,3 +348,29 @@ def test_prefill_values_that_are_not_finite_reach_only_who_attends_them(D):
     assert torch.allclose(rows[..., others], want, rtol=1e-6, atol=1e-6)
     free = ~hit_v & ~hit_k
     assert torch.allclose(out[0][free], clean[0][free], rtol=1e-6, atol=1e-6)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes_lengths_and_windows(seed):
+    """Seeded draws over heads, groups, batches, ragged lengths, windows, first
+    tokens and bounds: decode from either cache, and prefill."""
+    rng = np.random.default_rng(1000 + seed)
+    kind = ("4-bit", "bf16", "prefill")[seed % 3]
+    D = int(rng.choice([64, 128]))
+    g = int(rng.choice([1, 2, 3, 5]))
+    h = g * int(rng.choice([1, 2, 4, 7, 12, 20]))
+    B = int(rng.integers(1, 7))
+    most = int(np.exp(rng.uniform(np.log(4), np.log(2500))))
+    window = int(rng.choice([0, 1, int(rng.integers(1, most + 1)), int(rng.integers(1, 80))]))
+    sinks = int(rng.choice([0, 1, 4, int(rng.integers(0, 100))]))
+    T = int(rng.integers(2, 90)) if kind == "prefill" else 1
+    lens = T + rng.integers(0, most + 1, B) if T > 1 else rng.integers(0, most + 1, B)
+    S = (int(lens.max()) // 32 + int(rng.integers(1, 4))) * 32
+    label = f"random {seed} {kind} D{D} h{h} g{g} B{B} T{T} len<={most} w{window} s{sinks}"
+    say(label)
+    c = Case(kind == "4-bit", h, g, D, lens, S, 2000 + seed, k_scale=float(rng.choice([1, 3])), T=T,
+             window=window, sinks=sinks)
+    if T > 1:
+        c.check(c.prefill(), label, tokens=range(0, T, 5))
+    else:
+        c.check(c.decode(hint=int(rng.choice([0, max(1, int(lens.max()))]))), label)
