@@ -129,19 +129,28 @@ mlkv_status check_row_buffers(const void* k_rows, const void* v_rows) {
 
 // How a layer's (sequence, KV head) units are cut (span.hip): `chunks` parts of
 // the G query rows, runs of run_tiles tiles, at most `runs` of a unit.
-// runs: only as many as give every compute unit one workgroup of eight waves,
-// of at least two tiles a wave (us, on 256 such workgroups / 512 / 1024 of four
-// waves: 8 x 32768 tokens of four heads in 4 bits 16.0 / 17.8 / 19.1, 128 ragged
+// runs: as many as give every compute unit one workgroup of eight waves, of at
+// least two tiles a wave (us, on 256 such workgroups / 512 / 1024 of four waves:
+// 8 x 32768 tokens of four heads in 4 bits 16.0 / 17.8 / 19.1, 128 ragged
 // sequences 8.1 / 8.7 / 10.4, 4 x 16000 tokens of two heads of 128 channels
 // 11.8 / 14.9 / 15.0; runs of one tile a wave instead of two 7.0 -> 8.0 for two
-// windows of 4096).  Grids of more workgroups keep four waves: more of them are
-// resident at once (48 x 8 windows of 1023, 128 channels, bf16 43.8 / 45.3).
+// windows of 4096).  Where those workgroups, or the unsplit units, leave more
+// than a seventh of their rounds of the compute units idle, long units are cut
+// into up to kSpanFill workgroups of four waves a compute unit, of at least
+// kSpanLongTiles tiles (us, cut / not, 4 bits: 300 units of 4000 .. 32000 tokens
+// 83 / 129, 140 of 8000 .. 16000 31 / 43, 264 of 8000 35 / 45, 320 of 16000 with
+// 128 channels 128 / 135; bf16, 288 windows of 4096 117 / 134).  Fewer bf16
+// units than compute units stay whole: they reach the memory's rate as they are
+// (160 windows of 4096: 68 / 63).  Grids of more workgroups than compute units
+// take four waves, of which more are resident at once (48 x 8 windows of 1023,
+// 128 channels, bf16 43.8 / 45.3).
 struct SpanPlan {
   int chunks, chunk_rows, runs, run_tiles, waves;
   long units;
   size_t ml, need;  // offset of the (max, denominator) pairs, bytes in all; 0 without split runs
 };
-constexpr int kSpanMinTiles = 16;
+constexpr int kSpanMinTiles = 16, kSpanLongTiles = 32;
+constexpr long kSpanFill = 6;
 
 SpanPlan span_plan(const mlkv_map* map, int layer, int batch, int head_dim, bool four_bits,
                    int max_len, int window, int sinks) {
@@ -162,7 +171,14 @@ SpanPlan span_plan(const mlkv_map* map, int layer, int batch, int head_dim, bool
   long runs = cus / groups;
   const long longest = tiles / kSpanMinTiles;
   runs = runs < longest ? runs : longest;
-  pl.runs = static_cast<int>(runs < 1 ? 1 : runs);
+  runs = runs < 1 ? 1 : runs;
+  const long rounds = (groups * runs + cus - 1) / cus * cus;
+  if (20 * groups * runs < 17 * rounds && (four_bits || groups > cus)) {
+    long fill = kSpanFill * cus / groups;
+    fill = fill < tiles / kSpanLongTiles ? fill : tiles / kSpanLongTiles;
+    runs = runs > fill ? runs : fill;
+  }
+  pl.runs = static_cast<int>(runs);
   pl.run_tiles = (tiles + pl.runs - 1) / pl.runs;
   pl.waves = groups * pl.runs <= cus ? 8 : 4;
   if (pl.runs > 1) {

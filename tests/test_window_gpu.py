@@ -148,6 +148,17 @@ def test_decode_split_runs(four_bits, D, lens, window, sinks):
     assert torch.equal(bf16, out.bfloat16())
 
 
+@pytest.mark.parametrize("four_bits", [True, False])
+@pytest.mark.parametrize("D,B,g,window", [(64, 70, 4, 0), (64, 70, 4, 2100), (128, 35, 4, 0)])
+def test_more_long_sequences_than_compute_units(four_bits, D, B, g, window):
+    """Grids of several rounds of the compute units, whose long units are cut too."""
+    say(f"span rounds D={D} B={B} window={window} four_bits={four_bits}")
+    lens = np.array([(1, 2145, 40, 1100, 0, 2176, 2079, 300)[b % 8] for b in range(B)])
+    c = Case(four_bits, h=2 * g, g=g, D=D, lens=lens, S=2176, seed=83, window=window,
+             sinks=3 if window else 0)
+    c.check(c.decode(), "rounds")
+
+
 def test_lengths_above_the_hint_are_truncated_to_it():
     c = Case(True, 12, 1, 64, [300, 100], 320, 54)
     out = c.decode(hint=100)
