@@ -138,8 +138,9 @@ mlkv_status check_row_buffers(const void* k_rows, const void* v_rows) {
 // than a seventh of their rounds of the compute units idle, long units are cut
 // into up to kSpanFill workgroups of four waves a compute unit, of at least
 // kSpanLongTiles tiles (us, cut / not, 4 bits: 300 units of 4000 .. 32000 tokens
-// 83 / 129, 140 of 8000 .. 16000 31 / 43, 264 of 8000 35 / 45, 320 of 16000 with
-// 128 channels 128 / 135; bf16, 288 windows of 4096 117 / 134).  Fewer bf16
+// 81 / 129, 140 of 8000 .. 16000 30 / 43, 264 of 8000 34 / 45, 320 of 16000 with
+// 128 channels 125 / 134; bf16, 288 windows of 4096 114 / 134; from 16 tiles on
+// instead, 384 bf16 windows of 1023 take 45.6 for 41.9).  Fewer bf16
 // units than compute units stay whole: they reach the memory's rate as they are
 // (160 windows of 4096: 68 / 63).  Grids of more workgroups than compute units
 // take four waves, of which more are resident at once (48 x 8 windows of 1023,
