@@ -9,6 +9,21 @@
 // that none of its rows attends and masks those that not all of them do: with
 // w positions a row and t tokens a wave, about (w + t) / 32 tiles, of which
 // the 2 + t / 16 at the window's two edges are masked.
+//
+// Tiles go to LDS once a workgroup by direct loads, three of 64 channels or two
+// of 128 ahead of the one in use (bytes that leave 4 or 3 waves a SIMD); a wave
+// takes two blocks of 16 rows, which share each operand read (us, one block /
+// two, 2 sequences of 4096 tokens, 32 heads of 128 channels on 8, window 1024:
+// 187 / 148; three do not fit the registers; 32x32x16 products: 167).
+//
+// Bound by vector instructions and matrix products, which overlap only between
+// waves, and by q and out at each workgroup's ends: of the 143 us of that call
+// (119 GFLOP, 0.83 PFLOP/s; a large product reaches 1.38) the matrix cores are
+// busy in 43 %, vector issue in 56 % (110 instructions beside 34 products a
+// tile), and reading q and writing out, 134 MB, takes 32 by itself, since
+// workgroups of equal length reach their ends together.  8 sequences of 2000
+// tokens, 12 heads of 64 on one, window 256 (12 GFLOP, 53 MB): 28.6 us, of which
+// 14 are the ends.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
