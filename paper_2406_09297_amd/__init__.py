@@ -486,10 +486,18 @@ def _rows_arg(t: torch.Tensor, shape, device: int, name: str):
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
     B, T, heads, D = shape
     sb, st, sh, sd = t.stride()
-    row = st if T > 1 else sb if B > 1 else heads * D
-    if sd != 1 or (heads > 1 and sh != D) or (B > 1 and sb != T * row):
+    row = st if T > 1 else sb if T and B > 1 else heads * D
+    if T and (sd != 1 or (heads > 1 and sh != D) or (B > 1 and sb != T * row) or row > _INT_MAX):
         raise ValueError(f"{name}: rows must be contiguous and evenly spaced, strides {t.stride()}")
     return t.data_ptr(), row
+
+
+_INT_MAX = 2**31 - 1
+
+
+def _count(n: int, most: int) -> int:
+    """n as the C int that says the same: `most` and above alike, negative ones alike."""
+    return n if 0 <= n <= most else most if n > most else -1
 
 
 def _launch_device(device: int) -> int:
@@ -606,6 +614,8 @@ def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, ma
     device = _launch_device(cache._device)
     shape = (cache.batch, map_._heads, cache.head_dim)
     ws_ptr, ws_bytes = _ws_args(ws, device)
+    window, sinks = _count(window, _INT_MAX), _count(sinks, _INT_MAX)
+    max_len_hint = _count(max_len_hint, _INT_MAX)
     _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_._h,
              _arg(seq_lens, (shape[0],), torch.int32, device, "seq_lens"), window, sinks,
              _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint, ws_ptr,
@@ -641,7 +651,8 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
     shape = (cache.batch, q.shape[1], map_._heads, cache.head_dim)
     _check(lib().mlkv_prefill_attention_window(
         layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_.handle,
-        _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
+        _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1],
+        _count(window, _INT_MAX), _count(sinks, _INT_MAX),
         _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _stream(stream)))
 
 

@@ -305,3 +305,33 @@ def test_prompt_calls_on_a_stream_of_their_own_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_no_new_tokens_change_nothing(four_bits):
+    B, h, g, D, S = 3, 4, 2, 64, 64
+    mp = mlkv.Map.uniform(2, h, 1, g)
+    cache = (mlkv.QCache if four_bits else mlkv.Cache).empty(g, B, S, D)
+    planes = [cache.data] if four_bits else [cache.k, cache.v]
+    for p in planes:
+        p.fill_(3)
+    empty = lambda n: torch.empty((B, 0, n, D), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    mlkv.norm_rope_append(0, mp, cache, empty(h), empty(g), empty(g), lens, empty(h),
+                          rotary_dims=16)
+    if four_bits:
+        mlkv.qcache_append_rows(0, mp, cache, empty(g), empty(g), lens)
+    for p in planes:
+        assert (p == 3).all()
+
+
+def test_rows_further_apart_than_a_c_int_are_refused():
+    B, h, D = 2, 2, 64
+    mp = mlkv.Map.uniform(2, h, 1, 1)
+    cache = mlkv.Cache.empty(1, B, 32, D)
+    q = torch.empty(2 ** 32 + 256, dtype=torch.bfloat16, device="cuda").as_strided(
+        (B, 1, h, D), (2 ** 32, 2 ** 32, D, 1))
+    with pytest.raises(ValueError, match="evenly spaced"):
+        mlkv.norm_rope_append(1, mp, cache, q, None, None,
+                              torch.zeros(B, dtype=torch.int32, device="cuda"),
+                              torch.empty((B, 1, h, D), dtype=torch.bfloat16, device="cuda"))

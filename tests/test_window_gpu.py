@@ -385,3 +385,32 @@ def test_random_shapes_lengths_and_windows(seed):
         c.check(c.prefill(), label, tokens=range(0, T, 5))
     else:
         c.check(c.decode(hint=int(rng.choice([0, max(1, int(lens.max()))]))), label)
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_windows_and_sinks_beyond_a_c_int(four_bits):
+    """They say the same as the capacity; a negative one of any size is refused."""
+    c = Case(four_bits, 12, 2, 64, [70, 33], 96, 84)
+    want = c.decode()
+    for window, sinks in [(2 ** 32 + 5, 0), (5, 2 ** 32), (2 ** 63, 2 ** 31)]:
+        c.window, c.sinks = window, sinks
+        assert torch.equal(c.decode(), want)
+    c.window, c.sinks = 5, 0
+    with pytest.raises(mlkv.MLKVError, match="MLKV_ERR_CAPACITY"):
+        c.decode(hint=2 ** 32 + 40)
+    for window, sinks in [(-2 ** 32 - 1, 0), (-2 ** 32, 0), (5, -2 ** 32)]:
+        c.window, c.sinks = window, sinks
+        with pytest.raises(mlkv.MLKVError, match="MLKV_ERR_INVALID_ARG"):
+            c.decode()
+
+
+def test_prefill_windows_and_sinks_beyond_a_c_int():
+    c = Case(False, 12, 2, 64, [70, 33], 96, 85, T=5)
+    want = c.prefill()
+    for window, sinks in [(2 ** 32 + 5, 0), (5, 2 ** 32), (2 ** 63, 2 ** 31)]:
+        c.window, c.sinks = window, sinks
+        assert torch.equal(c.prefill(), want)
+    for window, sinks in [(-2 ** 32 - 1, 0), (-2 ** 32, 0), (5, -2 ** 32)]:
+        c.window, c.sinks = window, sinks
+        with pytest.raises(mlkv.MLKVError, match="MLKV_ERR_INVALID_ARG"):
+            c.prefill()
