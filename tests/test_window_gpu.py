@@ -221,6 +221,31 @@ def test_decode_captured_in_a_graph_follows_the_lengths(four_bits):
         assert torch.equal(out, c.decode())
 
 
+def test_two_graphs_share_a_workspace():
+    """Calls of other shapes, split into other runs, replayed in turn."""
+    say("two graphs, one workspace")
+    cases = [Case(True, 12, 2, 64, [3000, 5, 900], 3008, 86),
+             Case(False, 8, 4, 128, [1500, 2000], 2016, 87, window=1700, sinks=9)]
+    ws = max((c.ws for c in cases), key=lambda t: t.numel())
+    outs, graphs, want = [], [], []
+    for c in cases:
+        c.ws = ws
+        want.append(c.decode())
+        f = mlkv.qcache_decode_attention if c.four_bits else mlkv.decode_attention_window
+        outs.append(torch.empty_like(want[-1]))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            f(c.layer, c.q, c.cache, c.map, c.seq_lens, outs[-1], window=c.window, sinks=c.sinks,
+              ws=ws)
+    for turn in range(4):
+        for g, out, w, c in zip(graphs, outs, want, cases):
+            out.fill_(7.0)
+            g.replay()
+            assert torch.equal(out, w), turn
+            if turn % 2:
+                assert torch.equal(c.decode(), w)
+
+
 @pytest.mark.parametrize("L", [40, 700])
 def test_scores_that_are_all_minus_infinity_give_nan(L):
     """The quotient is 0 / 0; a sequence with one finite score has its value."""
