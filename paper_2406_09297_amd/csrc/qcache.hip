@@ -117,7 +117,21 @@ __device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, u16x8
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    const float inv = __builtin_amdgcn_rsqf(row_sum<D>(ss) * (1.f / D) + eps);
+    float mean = row_sum<D>(ss) * (1.f / D) + eps;
+    // Squares that leave fp32 at either end: the same row times a power of two
+    // (the quotient does not change).  A row's lanes take one side together.
+    if (!(mean < INFINITY) || mean < 0x1p-90f) {
+      const float scale = mean < 1.f ? 0x1p80f : 0x1p-80f;
+      ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] *= scale;
+        y[i] *= scale;
+        ss = fmaf(x[i], x[i], ss);
+      }
+      mean = row_sum<D>(ss) * (1.f / D) + eps * scale * scale;
+    }
+    const float inv = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] = x[i] * inv * ln.w[i];

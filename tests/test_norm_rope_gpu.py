@@ -335,3 +335,32 @@ def test_rows_further_apart_than_a_c_int_are_refused():
         mlkv.norm_rope_append(1, mp, cache, q, None, None,
                               torch.zeros(B, dtype=torch.int32, device="cuda"),
                               torch.empty((B, 1, h, D), dtype=torch.bfloat16, device="cuda"))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_rows_whose_squares_leave_fp32(D, eps):
+    """Rows up to bf16's largest and down to its smallest normal numbers, side
+    by side: a row times a power of two has the same norm where eps is small
+    beside it (below, the formula's 64 bits say what it has)."""
+    h, B = 6, 11
+    say(f"norm of extreme rows D={D} eps={eps}")
+    powers = np.array([125, 100, 64, 63, 30, 0, -30, -44, -46, -70, -118])
+    f = synth.bf16_to_f32(synth.normal_bf16(75, 0, (B, 1, h, D)))
+    f = np.clip(f, -3.9, 3.9)  # 3.9 2^125 < 2^127
+    f = np.where(np.abs(f) < 2.0 ** -8, np.float32(2.0 ** -8), f)  # normal numbers all
+    bits = synth.f32_to_bf16(np.ldexp(f, powers[:, None, None, None]).astype(np.float32))
+    w = _weight(3, D)
+    mp = mlkv.Map.uniform(2, h, 1, 1)
+    cache = mlkv.Cache.empty(1, B, 32, D)
+    q_out = torch.empty((B, 1, h, D), dtype=torch.bfloat16, device="cuda")
+    ctx = np.arange(B, dtype=np.int32)
+    mlkv.norm_rope_append(1, mp, cache, mlkv.bf16_tensor(bits, "cuda"), None, None,
+                          torch.from_numpy(ctx).cuda(), q_out, q_norm=mlkv.bf16_tensor(w, "cuda"),
+                          eps=eps, rotary_dims=32)
+    got = q_out.double().cpu().numpy()
+    for b in range(B):
+        if eps == 0 or powers[b] > -70:  # others leave bf16's normal numbers in the result
+            _check(got[b:b + 1], bits[b:b + 1], w, eps, 32, 10000.0, ctx[b:b + 1, None],
+                   f"row of 2^{powers[b]}")
+    assert np.isfinite(got).all()
