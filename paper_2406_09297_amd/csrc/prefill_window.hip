@@ -235,13 +235,14 @@ __device__ __forceinline__ void window_step(WaveState<D> (&st)[NB],
     }
   }
   weigh_rows<D, NB>(st, x, w.scale_log2, pf);
-  const int filled = Reach::below(w.L - first);
   const bool apart = APART && (ends || starts);
 #pragma unroll
   for (int n = 0; n < Tile<D>::DB / 4; ++n) {
     u16x8 v[4];
     tile->read_v(v, n, w.col, w.grp);
     if (t0 + kTile > w.L) {  // slots not filled yet may hold anything
+      int filled = Reach::below(w.L - first);
+      asm volatile("" : "+v"(filled));  // here: the masks are 30 instructions of every tile else
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = keep_filled(v[i], filled);
     }
