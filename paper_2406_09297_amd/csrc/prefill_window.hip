@@ -14,16 +14,17 @@
 // of 128 ahead of the one in use (bytes that leave 4 or 3 waves a SIMD); a wave
 // takes two blocks of 16 rows, which share each operand read (us, one block /
 // two, 2 sequences of 4096 tokens, 32 heads of 128 channels on 8, window 1024:
-// 187 / 148; three do not fit the registers; 32x32x16 products: 167).
+// 171 / 139; three do not fit the registers; 32x32x16 products 167 where these
+// took 148).
 //
-// Bound by vector instructions and matrix products, which overlap only between
-// waves, and by q and out at each workgroup's ends: of the 143 us of that call
-// (119 GFLOP, 0.83 PFLOP/s; a large product reaches 1.38) the matrix cores are
-// busy in 43 %, vector issue in 56 % (110 instructions beside 34 products a
-// tile), and reading q and writing out, 134 MB, takes 32 by itself, since
-// workgroups of equal length reach their ends together.  8 sequences of 2000
-// tokens, 12 heads of 64 on one, window 256 (12 GFLOP, 53 MB): 28.6 us, of which
-// 14 are the ends.
+// Bound by vector instructions, matrix products and LDS reads, which overlap
+// only between waves, and by q and out at each workgroup's ends: of the 137 us of
+// that call (119 GFLOP, 0.87 PFLOP/s; a large product reaches 1.38) the matrix
+// cores are busy in 46 %, vector issue in 52 % (72 instructions beside 34
+// products a tile), and reading q and writing out, 134 MB, takes 32 by itself,
+// since workgroups of equal length reach their ends together.  8 sequences of
+// 2000 tokens, 12 heads of 64 on one, window 256 (12 GFLOP, 53 MB): 28.3 us, of
+// which 14 are the ends, in one and a half rounds of resident workgroups.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
