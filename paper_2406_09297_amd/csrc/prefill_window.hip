@@ -17,8 +17,8 @@
 // 171 / 139; three do not fit the registers; 32x32x16 products 167 where these
 // took 148).
 //
-// Bound by vector instructions, matrix products and LDS reads, which overlap
-// only between waves, and by q and out at each workgroup's ends: of the 137 us of
+// Bound by vector instructions, matrix products and the waits for LDS, which
+// overlap only between waves, and by q and out at each workgroup's ends: of the 137 us of
 // that call (119 GFLOP, 0.87 PFLOP/s; a large product reaches 1.38) the matrix
 // cores are busy in 46 %, vector issue in 52 % (72 instructions beside 34
 // products a tile), and reading q and writing out, 134 MB, takes 32 by itself,
@@ -50,12 +50,12 @@ __device__ __forceinline__ void lds_read4(const uint16_t* at, u16x8 (&op)[4]) {
       reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) uint16_t*)at));
   asm volatile(
       "ds_read_b128 %0, %4\n\t"
-      "ds_read_b128 %1, %4 offset:1024\n\t"
-      "ds_read_b128 %2, %4 offset:2048\n\t"
-      "ds_read_b128 %3, %4 offset:3072\n\t"
+      "ds_read_b128 %1, %4 offset:%5\n\t"
+      "ds_read_b128 %2, %4 offset:%6\n\t"
+      "ds_read_b128 %3, %4 offset:%7\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(op[0]), "=&v"(op[1]), "=&v"(op[2]), "=&v"(op[3])
-      : "v"(off)
+      : "v"(off), "n"(1024), "n"(2 * 1024), "n"(3 * 1024)
       : "memory");
 #endif
 }
