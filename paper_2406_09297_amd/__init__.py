@@ -155,9 +155,12 @@ def _check(status: int):
         raise MLKVError(status, lib().mlkv_last_error().decode())
 
 
-def _stream(stream) -> int:
+def _stream(stream, device: int | None = None) -> int:
+    """Handle of `stream`, by default the current one of the current device
+    (`device`, where the caller knows it)."""
     if stream is None:  # the handle alone: a Stream object around it costs 2 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(
+            torch.cuda.current_device() if device is None else device)
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
@@ -485,9 +488,11 @@ def _rows_arg(t: torch.Tensor, shape, device: int, name: str):
         raise ValueError(f"{name} must be {tuple(shape)} in bfloat16 on cuda:{device}, got "
                          f"{tuple(t.shape)} {t.dtype} on {t.device}")
     B, T, heads, D = shape
+    if t.is_contiguous():
+        return t.data_ptr(), heads * D
     sb, st, sh, sd = t.stride()
-    row = st if T > 1 else sb if T and B > 1 else heads * D
-    if T and (sd != 1 or (heads > 1 and sh != D) or (B > 1 and sb != T * row) or row > _INT_MAX):
+    row = st if T > 1 else sb if B > 1 else heads * D
+    if (sd != 1 or (heads > 1 and sh != D) or (B > 1 and sb != T * row) or row > _INT_MAX):
         raise ValueError(f"{name}: rows must be contiguous and evenly spaced, strides {t.stride()}")
     return t.data_ptr(), row
 
@@ -495,9 +500,9 @@ def _rows_arg(t: torch.Tensor, shape, device: int, name: str):
 _INT_MAX = 2**31 - 1
 
 
-def _count(n: int, most: int) -> int:
-    """n as the C int that says the same: `most` and above alike, negative ones alike."""
-    return n if 0 <= n <= most else most if n > most else -1
+def _counts(*counts: int):
+    """The C ints that say the same: 2**31 - 1 and above alike, negative ones alike."""
+    return (n if 0 <= n <= _INT_MAX else _INT_MAX if n > 0 else -1 for n in counts)
 
 
 def _launch_device(device: int) -> int:
@@ -556,7 +561,7 @@ class QCache:
         device, at, shape = self._rows(starts, n, T)
         _check(lib().mlkv_qcache_write_rows(
             self.struct, kv_begin, n, at, T, _arg(k_rows, shape, torch.bfloat16, device, "k_rows"),
-            _arg(v_rows, shape, torch.bfloat16, device, "v_rows"), _stream(stream)))
+            _arg(v_rows, shape, torch.bfloat16, device, "v_rows"), _stream(stream, device)))
 
     def read_rows(self, kv_begin: int = 0, kv_count: int | None = None,
                   starts: torch.Tensor | None = None, T: int | None = None, stream=None):
@@ -564,12 +569,12 @@ class QCache:
         [kv_count][B][T][D]; T defaults to the capacity."""
         n = self.n_kv - kv_begin if kv_count is None else kv_count
         T = self.capacity if T is None else T
-        _, at, shape = self._rows(starts, n, T)
+        device, at, shape = self._rows(starts, n, T)
         k, v = torch.empty((2, *shape), dtype=torch.bfloat16, device=self.data.device).unbind()
         if isinstance(stream, torch.cuda.Stream):  # the rows are written there
             k.record_stream(stream)
         _check(lib().mlkv_qcache_read_rows(self.struct, kv_begin, n, at, T, k.data_ptr(),
-                                           v.data_ptr(), _stream(stream)))
+                                           v.data_ptr(), _stream(stream, device)))
         return k, v
 
 
@@ -597,7 +602,8 @@ def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor
     k, v, stride = _new_rows(layer, map_, cache, k_new, v_new, k_new.shape[1], device)
     _check(lib().mlkv_qcache_append_rows(
         layer, map_.handle, cache.struct, k, v, k_new.shape[1], stride,
-        _arg(ctx_lens, (cache.batch,), torch.int32, device, "ctx_lens"), _stream(stream)))
+        _arg(ctx_lens, (cache.batch,), torch.int32, device, "ctx_lens"),
+        _stream(stream, device)))
 
 
 def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda",
@@ -614,12 +620,12 @@ def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, ma
     device = _launch_device(cache._device)
     shape = (cache.batch, map_._heads, cache.head_dim)
     ws_ptr, ws_bytes = _ws_args(ws, device)
-    window, sinks = _count(window, _INT_MAX), _count(sinks, _INT_MAX)
-    max_len_hint = _count(max_len_hint, _INT_MAX)
+    if (window | sinks | max_len_hint) >> 31:  # some negative or beyond a C int
+        window, sinks, max_len_hint = _counts(window, sinks, max_len_hint)
     _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_._h,
              _arg(seq_lens, (shape[0],), torch.int32, device, "seq_lens"), window, sinks,
              _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint, ws_ptr,
-             ws_bytes, _stream(stream)))
+             ws_bytes, _stream(stream, device)))
 
 
 def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Map,
@@ -649,11 +655,12 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
     (fp32 or bf16); token t of sequence b stands at position ctx_lens[b] + t."""
     device = _launch_device(cache._device)
     shape = (cache.batch, q.shape[1], map_._heads, cache.head_dim)
+    if (window | sinks) >> 31:
+        window, sinks = _counts(window, sinks)
     _check(lib().mlkv_prefill_attention_window(
         layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_.handle,
-        _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1],
-        _count(window, _INT_MAX), _count(sinks, _INT_MAX),
-        _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _stream(stream)))
+        _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
+        _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _stream(stream, device)))
 
 
 def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch.Tensor | None,
@@ -685,7 +692,8 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
     f = L.mlkv_qcache_norm_rope_append if isinstance(cache, QCache) else L.mlkv_norm_rope_append
     _check(f(layer, map_.handle, cache.struct, qp, q_stride, kp, vp, stride, T,
              _arg(ctx_lens, (B,), torch.int32, device, "ctx_lens"), ctypes.byref(nr),
-             _arg(q_out, (B, T, h, D), torch.bfloat16, device, "q_out"), _stream(stream)))
+             _arg(q_out, (B, T, h, D), torch.bfloat16, device, "q_out"),
+             _stream(stream, device)))
 
 
 # ---------------------------------------------------------------- model ---

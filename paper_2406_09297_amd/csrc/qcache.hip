@@ -151,6 +151,10 @@ __device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, u16x8
   return out;
 }
 
+__device__ __forceinline__ double turns_of(const StoreParams& p, int j) {
+  return p.coarse[j >> 3] * p.fine[j & 7];
+}
+
 // cos and sin of pair j at position pos: the turns in 64 bits (a position of
 // 2^31 leaves 20 bits and more of its fraction), of which only the fraction
 // counts, then in 32.
@@ -198,7 +202,7 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
     const unsigned n_tok = (end - 1) / static_cast<unsigned>(p.h) + 1 - tok0;
     for (unsigned j = threadIdx.x; j < n_tok * p.half; j += kStoreThreads) {
       const unsigned i = j / p.half, g = tok0 + i, b = g / static_cast<unsigned>(p.T);
-      cs[j] = cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), p.turns[j - i * p.half]);
+      cs[j] = cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), turns_of(p, j - i * p.half));
     }
     __syncthreads();
   }
@@ -259,7 +263,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   if (NORM && p.half) {
     for (int j = threadIdx.x + u_lo * p.half; j < u_end * p.half; j += kStoreThreads) {
       const int u = j / p.half;
-      cs[j] = cos_sin(s0 + u, p.turns[j - u * p.half]);
+      cs[j] = cos_sin(s0 + u, turns_of(p, j - u * p.half));
     }
     __syncthreads();
   }

@@ -329,14 +329,11 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
   p.eps = static_cast<float>(nr->eps);
   // Revolutions base^(-2j / dims) / 2 pi, as the product of two powers each
   // (sixteen powers instead of up to 64, 3 us of a call).
-  double fine[8];
   for (int j = 0; j < 8 && j < p.half; ++j)
-    fine[j] = std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims);
-  for (int j = 0; j < p.half; j += 8) {
-    const double coarse =
+    p.fine[j] = std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims);
+  for (int j = 0; j < p.half; j += 8)
+    p.coarse[j / 8] =
         std::pow(nr->rotary_base, -2.0 * j / nr->rotary_dims) * 0.15915494309189533577;
-    for (int i = 0; i < 8; ++i) p.turns[j + i] = coarse * fine[i];
-  }
   return launch_store_checked(p, D, true, stream);
 }
 

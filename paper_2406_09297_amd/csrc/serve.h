@@ -47,7 +47,9 @@ struct StoreParams {
   unsigned q_rows, q_items;   // (token, head) rows of a query workgroup, and these workgroups
   int half;                   // rotated channel pairs (0: none)
   float eps;
-  double turns[kMaxRopePairs];  // revolutions a position turns pair j by
+  // A position turns pair j by coarse[j / 8] * fine[j % 8] revolutions (64
+  // products in the arguments cost 0.4 us a launch).
+  double coarse[kMaxRopePairs / 8], fine[8];
 };
 
 struct ReadParams {

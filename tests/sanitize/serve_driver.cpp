@@ -133,7 +133,7 @@ static void rows(int h, int g) {
             CHECK(p.half == D / 2);
             for (int j = 0; j < p.half; ++j) {
               const double want = pow(1e4, -2.0 * j / D) / (2 * M_PI);
-              CHECK(fabs(p.turns[j] - want) <= 4e-16 * want);
+              CHECK(fabs(p.coarse[j / 8] * p.fine[j % 8] - want) <= 4e-16 * want);
             }
           }
           if (static_cast<long>(T) * (h / g) <= 65535L * 128) {

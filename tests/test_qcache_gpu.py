@@ -139,3 +139,22 @@ def test_a_layer_without_heads_of_its_own_stores_nothing():
     mlkv.qcache_append_rows(1, mp, cache, rows, rows, ctx)
     torch.cuda.synchronize()
     assert np.array_equal(cache.data.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_rows_on_a_stream_of_their_own(as_handle):
+    """Written and read on a stream that is not the current one."""
+    D, B, S = 64, 2, 64
+    k, v = (mlkv.bf16_tensor(_awkward_rows(s, (1, B, S, D)), "cuda") for s in (41, 42))
+    cache, _ = _poisoned(1, B, S, D)
+    cache.write_rows(k, v)
+    want = cache.read_rows()
+    other = mlkv.QCache.empty(1, B, S, D)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    stream = side.cuda_stream if as_handle else side
+    other.write_rows(k, v, stream=stream)
+    got = other.read_rows(stream=stream)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(got, want):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
