@@ -439,3 +439,21 @@ def test_prefill_windows_and_sinks_beyond_a_c_int():
         c.window, c.sinks = window, sinks
         with pytest.raises(mlkv.MLKVError, match="MLKV_ERR_INVALID_ARG"):
             c.prefill()
+
+
+def test_prefill_captured_in_a_graph_follows_the_contexts():
+    c = Case(False, 12, 2, 64, [140, 90], 160, 88, T=40, window=33, sinks=2)
+    c.cache.k.nan_to_num_(0)
+    c.cache.v.nan_to_num_(0)
+    out = torch.empty(c.q.shape, dtype=torch.float32, device="cuda")
+    ctx = c.seq_lens - c.T
+    c.prefill()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mlkv.prefill_attention_window(c.layer, c.q, c.cache, c.map, ctx, out, window=33, sinks=2)
+    for lens in ([140, 90], [41, 160], [40, 40], [140, 90]):
+        c.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        ctx.copy_(c.seq_lens - c.T)
+        out.fill_(7.0)
+        graph.replay()
+        assert torch.equal(out, c.prefill())
