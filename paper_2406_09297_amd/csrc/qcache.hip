@@ -83,36 +83,41 @@ __device__ __forceinline__ float row_sum(float x) {
 template <int D>
 struct Lane {
   int c0, partner;    // partner: first channel of the other eight
+  int from;           // and the lane that has them, times 4
   bool normed, turned, hi;
-  float w[8], wp[8];
+  float w[8];
   __device__ __forceinline__ Lane(const uint16_t* weight, int c0_, int half) : c0(c0_) {
     turned = c0 < 2 * half;
     hi = c0 >= half;
     partner = !turned ? c0 : hi ? c0 - half : c0 + half;
+    from = 4 * ((static_cast<int>(threadIdx.x) & 63 & ~(D / 8 - 1)) + partner / 8);
     normed = weight != nullptr;
     if (normed) {
-      const u16x8 a = load16(weight + c0), b = load16(weight + partner);
+      const u16x8 a = load16(weight + c0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[i] = bf16_to_f32(a[i]);
-        wp[i] = bf16_to_f32(b[i]);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = bf16_to_f32(a[i]);
     }
   }
 };
 
+// Where a token's (cos, sin) of a pair stand in LDS: two pairs of each lane's
+// eight side by side, then the next two, so that a row's lanes read 16 bytes
+// each from neighbouring places (in the order of pairs, lanes are 64 bytes apart
+// and meet each other's banks: 2000 tokens on 4 sequences, 32 and 8 heads of
+// 128 channels, all turned, NBIG us).
+__device__ __forceinline__ int angle_place(int pair, int half) {
+  return (pair >> 1 & 3) * (half / 4) + (pair >> 3) * 2 + (pair & 1);
+}
+
 // A row's eight channels: divided by the row's root mean square and weighted,
-// then rotated with cs (cos, sin of the row's token from the lane's first pair
-// on), in fp32, rounded once to bf16.  All D / 8 lanes of a row take part.
+// then rotated with the angles at cs (those of the row's token) of the lane's
+// pairs, in fp32, rounded once to bf16.  All D / 8 lanes of a row take part.
 template <int D>
-__device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, u16x8 other, float eps,
-                                             const float2* cs) {
-  float x[8], y[8];
+__device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, float eps,
+                                             const float2* cs, int half) {
+  float x[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] = bf16_to_f32(raw[i]);
-    y[i] = bf16_to_f32(other[i]);
-  }
+  for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(raw[i]);
   if (ln.normed) {
     float ss = 0.f;
 #pragma unroll
@@ -126,23 +131,28 @@ __device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, u16x8
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] *= scale;
-        y[i] *= scale;
         ss = fmaf(x[i], x[i], ss);
       }
       mean = row_sum<D>(ss) * (1.f / D) + eps * scale * scale;
     }
     const float inv = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = x[i] * inv * ln.w[i];
-      y[i] = y[i] * inv * ln.wp[i];
-    }
+    for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * ln.w[i];
   }
-  if (ln.turned) {
+  if (half) {
+    float y[8];  // the channels that these are turned with, from their lane
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 t = cs[i];
-      x[i] = fmaf(x[i], t.x, ln.hi ? y[i] * t.y : -(y[i] * t.y));
+    for (int i = 0; i < 8; ++i)
+      y[i] = __builtin_bit_cast(
+          float, __builtin_amdgcn_ds_bpermute(ln.from, __builtin_bit_cast(int, x[i])));
+    if (ln.turned) {
+      const float2* at = cs + angle_place(ln.hi ? ln.partner : ln.c0, half);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float4 t = *reinterpret_cast<const float4*>(at + i / 2 * (half / 4));
+        x[i] = fmaf(x[i], t.x, ln.hi ? y[i] * t.y : -(y[i] * t.y));
+        x[i + 1] = fmaf(x[i + 1], t.z, ln.hi ? y[i + 1] * t.w : -(y[i + 1] * t.w));
+      }
     }
   }
   u16x8 out;
@@ -186,7 +196,7 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
   const unsigned total = static_cast<unsigned>(p.B) * p.T * p.h;
   const unsigned first = item * p.q_rows, end = min(first + p.q_rows, total);
   const Lane<D> ln(p.q_w, (threadIdx.x % C8) * 8, p.half);
-  u16x8 raw, other;
+  u16x8 raw;
   unsigned r = first + threadIdx.x / C8, tok, head;
   auto request = [&]() {
     const unsigned at = min(r, end - 1);  // rows past the end repeat the last one
@@ -194,7 +204,6 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
     head = at - tok * p.h;
     const uint16_t* row = p.q + tok * p.q_stride + head * D;
     raw = load16(row + ln.c0);
-    other = ln.turned ? load16(row + ln.partner) : raw;
   };
   request();
   const unsigned tok0 = first / static_cast<unsigned>(p.h);
@@ -202,17 +211,18 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
     const unsigned n_tok = (end - 1) / static_cast<unsigned>(p.h) + 1 - tok0;
     for (unsigned j = threadIdx.x; j < n_tok * p.half; j += kStoreThreads) {
       const unsigned i = j / p.half, g = tok0 + i, b = g / static_cast<unsigned>(p.T);
-      cs[j] = cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), turns_of(p, j - i * p.half));
+      const int pair = j - i * p.half;
+      cs[i * p.half + angle_place(pair, p.half)] =
+          cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), turns_of(p, pair));
     }
     __syncthreads();
   }
   for (unsigned r0 = first; r0 < end; r0 += ROWS) {
-    const u16x8 x = raw, y = other;
+    const u16x8 x = raw;
     const unsigned row = r, t = tok, hd = head;
     r += ROWS;
     if (r0 + ROWS < end) request();
-    const u16x8 out = norm_rotate<D>(ln, x, y, p.eps,
-                                     cs + (t - tok0) * p.half + (ln.hi ? ln.partner : ln.c0));
+    const u16x8 out = norm_rotate<D>(ln, x, p.eps, cs + (t - tok0) * p.half, p.half);
     if (row < end)
       *reinterpret_cast<u16x8*>(p.q_out + (static_cast<size_t>(t) * p.h + hd) * D + ln.c0) = out;
   }
@@ -224,7 +234,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   constexpr int ROWS = kStoreThreads / C8;  // token rows a pass of the workgroup takes
   constexpr int PASSES = kTile / ROWS;
   __shared__ StoreShared<D> sm;
-  __shared__ float2 cs[NORM ? kAngleTokens * kMaxRopePairs : 1];
+  alignas(16) __shared__ float2 cs[NORM ? kAngleTokens * kMaxRopePairs : 1];
   const unsigned item = item_of_block();
   if (item >= p.store_items) {
     if (NORM && item - p.store_items < p.q_items) norm_queries<D>(p, item - p.store_items, cs);
@@ -246,24 +256,23 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   const size_t seq = static_cast<size_t>(p.kv_begin + c) * p.B + b;
   uint8_t* const rec = Q4 ? p.q4 + (seq * (p.S / kTile) + s0 / kTile) * QTile<D>::kBytes : nullptr;
   const Lane<D> ln(NORM ? p.k_w : nullptr, c0, NORM ? p.half : 0);
-  u16x8 xk[PASSES], xv[PASSES], other[PASSES];
+  u16x8 xk[PASSES], xv[PASSES];
 #pragma unroll
   for (int pass = 0; pass < PASSES; ++pass) {
     const int u = pass * ROWS + row;
     const u16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-    xk[pass] = xv[pass] = other[pass] = zero;
+    xk[pass] = xv[pass] = zero;
     if (u >= u_lo && u < u_end) {
       const size_t src = static_cast<size_t>(c) * p.s_head + static_cast<size_t>(b) * p.s_seq +
                          static_cast<size_t>(s0 + u - start) * p.s_tok;
       xk[pass] = load16(p.k_src + src + c0);
       xv[pass] = load16(p.v_src + src + c0);
-      if (NORM && ln.turned) other[pass] = load16(p.k_src + src + ln.partner);
     }
   }
   if (NORM && p.half) {
     for (int j = threadIdx.x + u_lo * p.half; j < u_end * p.half; j += kStoreThreads) {
-      const int u = j / p.half;
-      cs[j] = cos_sin(s0 + u, turns_of(p, j - u * p.half));
+      const int u = j / p.half, pair = j - u * p.half;
+      cs[u * p.half + angle_place(pair, p.half)] = cos_sin(s0 + u, turns_of(p, pair));
     }
     __syncthreads();
   }
@@ -274,7 +283,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
     u16x8 k = xk[pass];
     const u16x8 v = xv[pass];
     if (NORM)
-      k = norm_rotate<D>(ln, k, other[pass], p.eps, cs + u * p.half + (ln.hi ? ln.partner : c0));
+      k = norm_rotate<D>(ln, k, p.eps, cs + u * p.half, p.half);
     if (Q4) {
       const int ek = block_exp(block_top(k)), ev = block_exp(block_top(v));
       const uint32_t nv = quantise8(v, ev);
