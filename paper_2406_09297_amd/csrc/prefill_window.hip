@@ -259,12 +259,6 @@ __device__ __forceinline__ void window_step(WaveState<D> (&st)[NB],
   }
 }
 
-// n / d for 0 <= n < 2^31 with inv = (2^32 - 1) / d: the estimate is at most one short.
-__device__ __forceinline__ int quotient(int n, int d, uint32_t inv) {
-  const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(n), inv));
-  return n - q * d >= d ? q + 1 : q;
-}
-
 // Chunk j (four channels) of a row of results staged in LDS; rows are permuted
 // so that lanes on the same chunk of 16 rows meet all banks.
 template <int D>

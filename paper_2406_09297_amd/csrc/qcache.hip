@@ -186,6 +186,13 @@ struct alignas(16) StoreShared {
   };
 };
 
+// j / p.half for the j < kAngleTokens * kMaxRopePairs < 2^12 angles of a
+// workgroup: the factor is above 2^20 / half by less than one, the product above
+// j 2^20 / half by less than 2^12, under one part in half.
+__device__ __forceinline__ int angle_token(const StoreParams& p, unsigned j) {
+  return static_cast<int>(__umul24(j, p.inv_half) >> 20);
+}
+
 // Queries: p.q_rows consecutive rows (token by token, head by head), the lanes
 // of a row side by side.  The first rows are requested ahead of the angles and
 // the next ones ahead of the arithmetic.
@@ -200,7 +207,7 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
   unsigned r = first + threadIdx.x / C8, tok, head;
   auto request = [&]() {
     const unsigned at = min(r, end - 1);  // rows past the end repeat the last one
-    tok = at / static_cast<unsigned>(p.h);
+    tok = quotient(at, p.h, p.inv_h);
     head = at - tok * p.h;
     const uint16_t* row = p.q + tok * p.q_stride + head * D;
     raw = load16(row + ln.c0);
@@ -210,7 +217,7 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
   if (p.half) {
     const unsigned n_tok = (end - 1) / static_cast<unsigned>(p.h) + 1 - tok0;
     for (unsigned j = threadIdx.x; j < n_tok * p.half; j += kStoreThreads) {
-      const unsigned i = j / p.half, g = tok0 + i, b = g / static_cast<unsigned>(p.T);
+      const unsigned i = angle_token(p, j), g = tok0 + i, b = g / static_cast<unsigned>(p.T);
       const int pair = j - i * p.half;
       cs[i * p.half + angle_place(pair, p.half)] =
           cos_sin(static_cast<long>(p.starts[b]) + (g - b * p.T), turns_of(p, pair));
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   }
   if (NORM && p.half) {
     for (int j = threadIdx.x + u_lo * p.half; j < u_end * p.half; j += kStoreThreads) {
-      const int u = j / p.half, pair = j - u * p.half;
+      const int u = angle_token(p, j), pair = j - u * p.half;
       cs[u * p.half + angle_place(pair, p.half)] = cos_sin(s0 + u, turns_of(p, pair));
     }
     __syncthreads();

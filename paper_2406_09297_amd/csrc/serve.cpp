@@ -325,7 +325,9 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
   p.q_items = static_cast<unsigned>((total + p.q_rows - 1) / p.q_rows);
   if (static_cast<double>(p.store_items) + p.q_items > 2147483647.0)
     return fail(MLKV_ERR_CAPACITY, "more than 2^31 - 1 workgroups in one call");
+  p.inv_h = 0xFFFFFFFFu / static_cast<uint32_t>(h);
   p.half = nr->rotary_dims / 2;
+  p.inv_half = p.half ? ((1u << 20) + p.half - 1) / p.half : 0;
   p.eps = static_cast<float>(nr->eps);
   // Revolutions base^(-2j / dims) / 2 pi, as the product of two powers each
   // (sixteen powers instead of up to 64, 3 us of a call).

@@ -45,7 +45,9 @@ struct StoreParams {
   size_t q_stride;
   int h;
   unsigned q_rows, q_items;   // (token, head) rows of a query workgroup, and these workgroups
+  uint32_t inv_h;             // (2^32 - 1) / h
   int half;                   // rotated channel pairs (0: none)
+  unsigned inv_half;          // 2^20 / half, rounded up
   float eps;
   // A position turns pair j by coarse[j / 8] * fine[j % 8] revolutions (64
   // products in the arguments cost 0.4 us a launch).

@@ -59,6 +59,12 @@ __device__ __forceinline__ f32x4 load4_device(__amdgpu_buffer_rsrc_t r, uint32_t
   return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kCpolDevice));
 }
 
+// n / d for 0 <= n < 2^31 with inv = (2^32 - 1) / d: the estimate is at most one short.
+__device__ __forceinline__ int quotient(int n, int d, uint32_t inv) {
+  const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(n), inv));
+  return n - q * d >= d ? q + 1 : q;
+}
+
 __device__ __forceinline__ uint16_t f32_to_bf16_bits(float f) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));
 }
