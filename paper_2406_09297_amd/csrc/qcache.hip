@@ -26,8 +26,9 @@
 //   8 sequences of 2000 rows of 4 heads of 64 (20.7 MB)             5.8, 3.6 TB/s
 //   one row of each of 128 sequences                                2.8
 //   norm and rotation, bf16 cache, 8 sequences of 2000 rows, 12
-//   query and 4 KV heads of 64 (82 MB)                             18.4, 4.4 TB/s
-//   one row of each of 64 sequences, 32 and 8 heads of 128          6.4
+//   query and 4 KV heads of 64 (82 MB)                             17.7, 4.6 TB/s
+//   4 sequences of 2000, 32 and 8 heads of 128, all turned (197 MB) 47, 4.2 TB/s
+//   one row of each of 64 sequences, the same heads               6.2
 // (a copy of 0.5 to 4 GB reaches 4.6 to 5.3 TB/s, read and written).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -79,7 +80,8 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // What a thread needs for its channels c0 .. c0 + 7 of every row: their norm
-// weights and those of the channels they are turned with.
+// weights and the lane that has the channels they are turned with (fetched from
+// it after its norm; reading and norming them twice took a tenth longer).
 template <int D>
 struct Lane {
   int c0, partner;    // partner: first channel of the other eight
@@ -103,8 +105,8 @@ struct Lane {
 // Where a token's (cos, sin) of a pair stand in LDS: two pairs of each lane's
 // eight side by side, then the next two, so that a row's lanes read 16 bytes
 // each from neighbouring places (in the order of pairs, lanes are 64 bytes apart
-// and meet each other's banks: 2000 tokens on 4 sequences, 32 and 8 heads of
-// 128 channels, all turned, NBIG us).
+// and meet each other's banks: one token on 256 sequences, 32 and 8 heads of
+// 128 channels, all turned, 12.7 us; so, 11.0).
 __device__ __forceinline__ int angle_place(int pair, int half) {
   return (pair >> 1 & 3) * (half / 4) + (pair >> 3) * 2 + (pair & 1);
 }
@@ -176,9 +178,12 @@ __device__ __forceinline__ float2 cos_sin(long pos, double turns) {
   return make_float2(c, s);
 }
 
-template <int D>
+// The angles are done with when the values come (one place for both: eight
+// waves a SIMD instead of six with 128 channels, 11.0 -> 10.0 us for that token).
+template <int D, bool NORM>
 struct alignas(16) StoreShared {
   union {
+    float2 cs[NORM ? kAngleTokens * (D / 2) : 1];
     uint32_t nib[kTile * D / 4];       // value codes, a byte each: [token][channel]
     // Values: [token][channel]; rows four elements longer, so that the lanes
     // that read four groups of eight tokens meet four sets of banks.
@@ -240,8 +245,8 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   constexpr int C8 = D / 8;
   constexpr int ROWS = kStoreThreads / C8;  // token rows a pass of the workgroup takes
   constexpr int PASSES = kTile / ROWS;
-  __shared__ StoreShared<D> sm;
-  alignas(16) __shared__ float2 cs[NORM ? kAngleTokens * kMaxRopePairs : 1];
+  __shared__ StoreShared<D, NORM> sm;
+  float2* const cs = sm.cs;
   const unsigned item = item_of_block();
   if (item >= p.store_items) {
     if (NORM && item - p.store_items < p.q_items) norm_queries<D>(p, item - p.store_items, cs);
@@ -286,29 +291,35 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
 #pragma unroll
   for (int pass = 0; pass < PASSES; ++pass) {
     const int u = pass * ROWS + row;
-    const bool live = u >= u_lo && u < u_end;
     u16x8 k = xk[pass];
-    const u16x8 v = xv[pass];
-    if (NORM)
-      k = norm_rotate<D>(ln, k, p.eps, cs + u * p.half, p.half);
+    if (NORM) k = norm_rotate<D>(ln, k, p.eps, cs + u * p.half, p.half);
     if (Q4) {
-      const int ek = block_exp(block_top(k)), ev = block_exp(block_top(v));
-      const uint32_t nv = quantise8(v, ev);
+      const int e = block_exp(block_top(k));
+      if (u >= u_lo && u < u_end) {
+        *reinterpret_cast<uint32_t*>(rec + QTile<D>::k_dword(u, c8)) = quantise8(k, e);
+        if (c8 % 4 == 0) rec[QTile<D>::k_exp(u, c8 / 4)] = static_cast<uint8_t>(e);
+      }
+    } else if (u >= u_lo && u < u_end) {
+      *reinterpret_cast<u16x8*>(p.k + (seq * p.S + s0) * D + kchunk<D>(u, c8) * 8) = k;
+    }
+  }
+  if (NORM && p.half) __syncthreads();  // the angles' place is the values'
+#pragma unroll
+  for (int pass = 0; pass < PASSES; ++pass) {
+    const int u = pass * ROWS + row;
+    const u16x8 v = xv[pass];
+    if (Q4) {
+      const int e = block_exp(block_top(v));
+      const uint32_t nv = quantise8(v, e);
       // Nibbles 0 .. 3 and 4 .. 7 to bytes.
       uint32_t lo4 = nv & 0xFFFF, hi4 = nv >> 16;
       lo4 = (lo4 | lo4 << 8) & 0x00FF00FF;
       hi4 = (hi4 | hi4 << 8) & 0x00FF00FF;
       sm.nib[(u * D + c0) / 4] = (lo4 | lo4 << 4) & 0x0F0F0F0F;
       sm.nib[(u * D + c0) / 4 + 1] = (hi4 | hi4 << 4) & 0x0F0F0F0F;
-      if (live) {
-        *reinterpret_cast<uint32_t*>(rec + QTile<D>::k_dword(u, c8)) = quantise8(k, ek);
-        if (c8 % 4 == 0) {
-          rec[QTile<D>::k_exp(u, c8 / 4)] = static_cast<uint8_t>(ek);
-          rec[QTile<D>::v_exp(u, c8 / 4)] = static_cast<uint8_t>(ev);
-        }
-      }
+      if (u >= u_lo && u < u_end && c8 % 4 == 0)
+        rec[QTile<D>::v_exp(u, c8 / 4)] = static_cast<uint8_t>(e);
     } else {
-      if (live) *reinterpret_cast<u16x8*>(p.k + (seq * p.S + s0) * D + kchunk<D>(u, c8) * 8) = k;
       const uint4 d = __builtin_bit_cast(uint4, v);
       *reinterpret_cast<uint2*>(&sm.val[u][c0]) = make_uint2(d.x, d.y);
       *reinterpret_cast<uint2*>(&sm.val[u][c0 + 4]) = make_uint2(d.z, d.w);
