@@ -264,6 +264,9 @@ mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, con
   return ok();
 }
 
+// Passes of a query workgroup (below; us, 16000 tokens of 12 and 4 heads of 64
+// channels, all turned, with 8 / 4 / 16 workgroups a compute unit 18.2 / 19.5 /
+// 18.7; 8000 of 32 and 8 heads of 128 with at most 4 / 8 passes 45.8 / 47.5).
 constexpr long kQueryGroupsPerCu = 8, kMaxQueryPasses = 4;
 
 mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* bf16,
