@@ -226,7 +226,7 @@ def _pack(x):
     b = x.float().unflatten(-1, (-1, 32))
     top = b.abs().amax(-1, keepdim=True)
     mantissa, exponent = torch.frexp(top)  # top = mantissa 2^exponent, mantissa in [0.5, 1)
-    e = (exponent - 3 + (mantissa >= 0.875)).clamp(-124, 125)
+    e = (exponent - 3 + (mantissa >= 0.875)).clamp(-125, 125)
     m = torch.ldexp(b.abs(), -e)
     code = ((m > 0.25).byte() + (m >= 0.75) + (m > 1.25) + (m >= 1.75) + (m > 2.5) + (m >= 3.5)
             + (m > 5.0)) | (torch.signbit(b).byte() << 3)
@@ -353,9 +353,9 @@ def _held(x):
     x = x.double()
     blocks = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
     top = blocks.abs().max(-1, keepdim=True).values
-    e = torch.where(top > 0, torch.floor(torch.log2(top.clamp(min=2.0 ** -140) / 7)) + 1, -124.0)
+    e = torch.where(top > 0, torch.floor(torch.log2(top.clamp(min=2.0 ** -140) / 7)) + 1, -125.0)
     e = torch.where(top < 7 * torch.exp2(e - 1), e - 1, e)
-    e = torch.where(top >= 7 * torch.exp2(e), e + 1, e).clamp(-124, 125)
+    e = torch.where(top >= 7 * torch.exp2(e), e + 1, e).clamp(-125, 125)
     y = blocks / torch.exp2(e)
     step = torch.where(y.abs() < 2, 0.5, torch.where(y.abs() < 4, 1.0, 2.0))
     return (torch.round(y / step) * step * torch.exp2(e)).reshape(x.shape)
