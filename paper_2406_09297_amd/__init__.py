@@ -166,6 +166,31 @@ def _stream(stream, device: int | None = None) -> int:
     return int(stream)
 
 
+def _write_on(stream, made, call, device: int | None = None):
+    """call(handle of `stream`), where the tensors `made` were just allocated and
+    the call writes them: behind what the current stream, whose memory they are,
+    still does with former tensors there, and before it goes to others."""
+    if stream is None:
+        return call(_stream(None, device))
+    at = made[0].device
+    current = torch.cuda.current_stream(at)
+    if isinstance(stream, torch.cuda.Stream):
+        if stream != current:
+            stream.wait_stream(current)
+            for t in made:
+                t.record_stream(stream)
+        return call(stream.cuda_stream)
+    # A bare handle's stream may be gone before the tensors are: the current
+    # stream waits for it instead of the allocator.
+    if int(stream) == current.cuda_stream:
+        return call(int(stream))
+    side = (torch.cuda.ExternalStream(int(stream), device=at) if int(stream)
+            else torch.cuda.default_stream(at))
+    side.wait_stream(current)
+    call(int(stream))
+    current.wait_stream(side)
+
+
 def _dev_ptr(t: torch.Tensor, dtype, name: str) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -323,8 +348,9 @@ class Cache:
         shape = (n, self.batch, self.capacity, self.head_dim)
         k = torch.empty(shape, dtype=torch.bfloat16, device=self.k.device)
         v = torch.empty(shape, dtype=torch.bfloat16, device=self.k.device)
-        _check(lib().mlkv_cache_read_rows(self.struct, kv_begin, n, _dev_ptr(k, torch.bfloat16, "k"),
-                                          _dev_ptr(v, torch.bfloat16, "v"), _stream(stream)))
+        _write_on(stream, (k, v), lambda handle: _check(lib().mlkv_cache_read_rows(
+            self.struct, kv_begin, n, _dev_ptr(k, torch.bfloat16, "k"),
+            _dev_ptr(v, torch.bfloat16, "v"), handle)))
         return k, v
 
     def load_rows(self, k_rows: np.ndarray, v_rows: np.ndarray, kv_range=None):
@@ -354,8 +380,13 @@ def workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda"
     """Allocate and initialise (mlkv_workspace_init) a decode workspace (with
     room for the rotary table of mlkv_decode_step_rope when rotary_dims > 0)."""
     n = map_.workspace_bytes(batch, capacity, head_dim, rotary_dims)
+    return _initialised(n, device, stream)
+
+
+def _initialised(n: int, device, stream) -> torch.Tensor:
     ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
-    _check(lib().mlkv_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)))
+    _write_on(stream, (ws,), lambda handle: _check(
+        lib().mlkv_workspace_init(ws.data_ptr(), ws.numel(), handle)))
     return ws
 
 
@@ -571,10 +602,9 @@ class QCache:
         T = self.capacity if T is None else T
         device, at, shape = self._rows(starts, n, T)
         k, v = torch.empty((2, *shape), dtype=torch.bfloat16, device=self.data.device).unbind()
-        if isinstance(stream, torch.cuda.Stream):  # the rows are written there
-            k.record_stream(stream)
-        _check(lib().mlkv_qcache_read_rows(self.struct, kv_begin, n, at, T, k.data_ptr(),
-                                           v.data_ptr(), _stream(stream, device)))
+        _write_on(stream, (k,), lambda handle: _check(lib().mlkv_qcache_read_rows(
+            self.struct, kv_begin, n, at, T, k.data_ptr(), v.data_ptr(), handle)),
+            device)
         return k, v
 
 
@@ -610,9 +640,7 @@ def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device
                      stream=None) -> torch.Tensor:
     """Allocate and initialise a workspace of mlkv_workspace_bytes_window bytes."""
     n = lib().mlkv_workspace_bytes_window(map_.handle, batch, capacity, head_dim)
-    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
-    _check(lib().mlkv_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)))
-    return ws
+    return _initialised(n, device, stream)
 
 
 def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, max_len_hint, ws,
