@@ -49,7 +49,10 @@ def world(monkeypatch):
         return mlkv.MLKV_OK
 
     library = types.SimpleNamespace(
-        mlkv_cache_read_rows=launch, mlkv_qcache_read_rows=launch, mlkv_workspace_init=launch,
+        **{name: launch for name in mlkv.EXPORTS if name.startswith("mlkv_qcache_")
+           or name.endswith("_window") or name == "mlkv_norm_rope_append"})
+    library.__dict__.update(
+        mlkv_cache_read_rows=launch, mlkv_workspace_init=launch,
         mlkv_workspace_bytes=lambda *a: 64, mlkv_workspace_bytes_window=lambda *a: 64)
     monkeypatch.setattr(mlkv, "lib", lambda: library)
     return types.SimpleNamespace(log=log, current=current, side=FakeStream(SIDE, log))
@@ -89,3 +92,40 @@ def test_what_a_call_allocates_is_written_in_order(make, world):
         make(handle)
         assert world.log == [("empty",)] * made + [("wait", handle, CURRENT), ("launch", handle),
                                                    ("wait", CURRENT, handle)]
+
+
+def _calls():
+    """Every long-context call whose tensors the caller has made, on fakes."""
+    B, h, D, S = 1, 2, 64, 32
+    mp = types.SimpleNamespace(handle=None, _h=None, _heads=h, _owned=[1])
+    bf16 = dict(dtype=torch.bfloat16)
+    q, rows, lens = torch.zeros((B, h, D), **bf16), torch.zeros((1, B, S, D), **bf16), \
+        torch.zeros(B, dtype=torch.int32)
+    q4, new = torch.zeros((B, 1, h, D), **bf16), torch.zeros((B, 1, 1, D), **bf16)
+    four, two = _cache(mlkv.QCache), _cache(mlkv.Cache)
+    return [
+        lambda s: four.write_rows(rows, rows, stream=s),
+        lambda s: mlkv.qcache_append_rows(0, mp, four, new, new, lens, stream=s),
+        lambda s: mlkv.qcache_decode_attention(0, q, four, mp, lens, q, stream=s),
+        lambda s: mlkv.decode_attention_window(0, q, two, mp, lens, q, 8, stream=s),
+        lambda s: mlkv.prefill_attention_window(0, q4, two, mp, lens, q4, 8, stream=s),
+        lambda s: mlkv.norm_rope_append(0, mp, two, q4, new, new, lens, q4, stream=s),
+        lambda s: mlkv.norm_rope_append(0, mp, four, q4, new, new, lens, q4, stream=s)]
+
+
+@pytest.mark.parametrize("n", range(7))
+def test_a_call_on_another_stream_comes_after_its_tensors(n, world, monkeypatch):
+    """A torch Stream waits for the current one, which made the arguments; a
+    bare handle and the current stream itself are launched on as they are."""
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    call = _calls()[n]
+    world.log.clear()
+    for stream, handle in ((None, CURRENT), (world.current, CURRENT), (CURRENT, CURRENT),
+                           (SIDE, SIDE)):
+        call(stream)
+        assert world.log == [("launch", handle)]
+        world.log.clear()
+    call(world.side)
+    assert world.log == [("wait", SIDE, CURRENT), ("launch", SIDE)]
+    with pytest.raises(ValueError, match="stream on device 1"):
+        call(FakeStream(SIDE, world.log, device_index=1))
