@@ -166,17 +166,21 @@ def _stream(stream, device: int | None = None) -> int:
     return int(stream)
 
 
-def _call_stream(stream, device: int) -> int:
-    """Handle of the stream of a call whose tensors the caller made.  A torch Stream
-    that is not the current one first waits for what the current one was given:
-    fills and temporaries (`ctx + 1` in the call itself) come from there, and the
-    caller could not order them any later.  A bare handle is taken as it is."""
+def _call_stream(stream, device: int, *tensors) -> int:
+    """Handle of the stream of a call on the caller's `tensors` (or None).  A torch
+    Stream that is not the current one first waits for what the current one was
+    given: fills and temporaries (`ctx + 1` in the call itself) come from there, and
+    the caller could not order them any later; their memory is not given away
+    before the call is done with it.  A bare handle is taken as it is."""
     if isinstance(stream, torch.cuda.Stream):
         if stream.device_index != device:
             raise ValueError(f"stream on device {stream.device_index}, tensors on device {device}")
         current = torch.cuda.current_stream(device)
         if stream != current:
             stream.wait_stream(current)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
         return stream.cuda_stream
     return _stream(stream, device)
 
@@ -607,7 +611,8 @@ class QCache:
         device, at, shape = self._rows(starts, n, T)
         _check(lib().mlkv_qcache_write_rows(
             self.struct, kv_begin, n, at, T, _arg(k_rows, shape, torch.bfloat16, device, "k_rows"),
-            _arg(v_rows, shape, torch.bfloat16, device, "v_rows"), _call_stream(stream, device)))
+            _arg(v_rows, shape, torch.bfloat16, device, "v_rows"),
+            _call_stream(stream, device, k_rows, v_rows, starts)))
 
     def read_rows(self, kv_begin: int = 0, kv_count: int | None = None,
                   starts: torch.Tensor | None = None, T: int | None = None, stream=None):
@@ -648,7 +653,7 @@ def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor
     _check(lib().mlkv_qcache_append_rows(
         layer, map_.handle, cache.struct, k, v, k_new.shape[1], stride,
         _arg(ctx_lens, (cache.batch,), torch.int32, device, "ctx_lens"),
-        _call_stream(stream, device)))
+        _call_stream(stream, device, k_new, v_new, ctx_lens)))
 
 
 def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda",
@@ -668,7 +673,7 @@ def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, ma
     _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_._h,
              _arg(seq_lens, (shape[0],), torch.int32, device, "seq_lens"), window, sinks,
              _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint, ws_ptr,
-             ws_bytes, _call_stream(stream, device)))
+             ws_bytes, _call_stream(stream, device, q, seq_lens, out, ws)))
 
 
 def qcache_decode_attention(layer: int, q: torch.Tensor, cache: QCache, map_: Map,
@@ -703,7 +708,8 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
     _check(lib().mlkv_prefill_attention_window(
         layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_.handle,
         _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
-        _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), _call_stream(stream, device)))
+        _arg(out, shape, out.dtype, device, "out"), _out_dtype(out),
+        _call_stream(stream, device, q, ctx_lens, out)))
 
 
 def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch.Tensor | None,
@@ -736,7 +742,7 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
     _check(f(layer, map_.handle, cache.struct, qp, q_stride, kp, vp, stride, T,
              _arg(ctx_lens, (B,), torch.int32, device, "ctx_lens"), ctypes.byref(nr),
              _arg(q_out, (B, T, h, D), torch.bfloat16, device, "q_out"),
-             _call_stream(stream, device)))
+             _call_stream(stream, device, q, k_new, v_new, ctx_lens, q_norm, k_norm, q_out)))
 
 
 # ---------------------------------------------------------------- model ---

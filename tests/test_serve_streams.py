@@ -115,8 +115,9 @@ def _calls():
 
 @pytest.mark.parametrize("n", range(7))
 def test_a_call_on_another_stream_comes_after_its_tensors(n, world, monkeypatch):
-    """A torch Stream waits for the current one, which made the arguments; a
-    bare handle and the current stream itself are launched on as they are."""
+    """A torch Stream waits for the current one, which made the arguments, and the
+    allocator keeps their memory for it; a bare handle and the current stream itself
+    are launched on as they are."""
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
     call = _calls()[n]
     world.log.clear()
@@ -126,6 +127,8 @@ def test_a_call_on_another_stream_comes_after_its_tensors(n, world, monkeypatch)
         assert world.log == [("launch", handle)]
         world.log.clear()
     call(world.side)
-    assert world.log == [("wait", SIDE, CURRENT), ("launch", SIDE)]
+    kept = world.log.count(("record", SIDE))  # the tensors passed, whatever becomes of them after
+    assert kept == (2, 3, 3, 3, 3, 5, 5)[n]
+    assert world.log == [("wait", SIDE, CURRENT)] + [("record", SIDE)] * kept + [("launch", SIDE)]
     with pytest.raises(ValueError, match="stream on device 1"):
         call(FakeStream(SIDE, world.log, device_index=1))
