@@ -447,6 +447,9 @@ mlkv_status mlkv_qcache_read_rows(const mlkv_qcache* cache, int kv_begin, int kv
  * zeros.  Any number of query heads per KV head.
  * mlkv_qcache_decode_attention reads the 4-bit cache: keys and values are
  * exactly those held.
+ * Softmax weights (in 4 bits also times a value block's 2^e) are rounded to bf16,
+ * sums held in fp32.  Values up to bf16's largest are in range for up to 2^24
+ * positions; beside the rounding a result may be off by L_b * 2^-91 * max(1, |v|).
  *   max_len_hint: as mlkv_decode_attention (lengths above it are truncated).
  *   workspace: device memory of at least mlkv_workspace_bytes_window(...)
  *        bytes, 16-byte aligned, initialised once by mlkv_workspace_init; it

@@ -18,7 +18,8 @@
 // an operand's eight codes are eight tokens of one channel, each with a scale
 // of its own, so the scale goes to the other operand: the weights times 2^e of
 // their token, one set per block of 32 channels, rounded to bf16 as the
-// denominator's weights are (a power of two changes no rounding).
+// denominator's weights are (a power of two changes no rounding, and with weights
+// <= 2^-24 none of the format's 2^e overflows; products below 2^-126 lose bits).
 //
 // Bound by reading the cache.  A tile is read once, straight into the registers
 // of the wave that needs it, 1 KB a load in operand order, so nothing passes

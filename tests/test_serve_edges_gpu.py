@@ -46,3 +46,33 @@ def test_split_runs_on_another_stream(four_bits, as_handle):
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(out, want)
         assert not c.ws[:262144].any()
+
+
+@pytest.mark.parametrize("kind", ["4-bit", "bf16", "prefill"])
+@pytest.mark.parametrize("D,power", [(64, 125), (128, 121), (64, 119), (64, -40)])
+def test_values_near_the_ends_of_bf16(kind, D, power):
+    """Values of up to 1.5 * 2^power, among them rows of zeros, with scores that
+    climb by less than the step at which a softmax reference moves: the results
+    are finite and within the bound of any other values.  power 125: rows of
+    1.5 * 2^126 all alike, whose sum alone leaves fp32."""
+    say(f"values near 2^{power}, {kind}, D={D}")
+    T = 40 if kind == "prefill" else 1
+    c = Case(kind == "4-bit", 4, 1, D, [300, 200], 320, 91, T=T)
+    g = np.random.default_rng(abs(power))
+    shape = (1, 2, 320, D)
+    # Scores q.k / sqrt(D) of 0 .. 5 (7.2 in log2): channel 0 climbs with the position.
+    k = np.zeros(shape, np.float32)
+    k[..., 0] = np.linspace(0, 5 * np.sqrt(D), 320)[None, None]
+    k[..., 1:] = g.normal(0, 0.01, (1, 2, 320, D - 1))
+    v = g.uniform(0.5, 1.5, shape) * np.where(g.random(shape) < 0.5, -1, 1)
+    v[:, :, ::7] = 0
+    v[0, 1] = 1.5 if power != 125 else 3.0
+    k, v = synth.f32_to_bf16(k), synth.f32_to_bf16(np.ldexp(v, power).astype(np.float32))
+    q = synth.bf16_to_f32(c.q_bits).copy()
+    q[..., 0] = 1.0
+    c.q_bits = synth.f32_to_bf16(q)
+    c.q = mlkv.bf16_tensor(c.q_bits, "cuda")
+    c.cache.write_rows(mlkv.bf16_tensor(k, "cuda"), mlkv.bf16_tensor(v, "cuda"), 1)
+    held = serve_ref.held if kind == "4-bit" else serve_ref.f64
+    c.k, c.v = held(k), held(v)
+    c.check(c.prefill() if T > 1 else c.decode(), f"values near 2^{power}")
