@@ -336,7 +336,10 @@ void span_kernel(SpanParams p) {
     if (slot < 0) {
       // A row that attends nothing is zero; one whose scores are all -inf has a
       // denominator of zero too, and is NaN.
-      const f32x4 y = sp.L > 0 ? o * __builtin_amdgcn_rcpf(den) : f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 y = sp.L > 0 ? o * __builtin_amdgcn_rcpf(den) : f32x4{0.f, 0.f, 0.f, 0.f};
+      // Held values are finite or NaN, and so are their sums (kLead): an infinite
+      // one comes from an exponent byte of 255, which scales weights by inf here.
+      if constexpr (Q4) y += o * 0.f;
       store4_as<D>(p.out, p.out_bf16, out_row + rr, d, y);
       return;
     }

@@ -76,3 +76,27 @@ def test_values_near_the_ends_of_bf16(kind, D, power):
     held = serve_ref.held if kind == "4-bit" else serve_ref.f64
     c.k, c.v = held(k), held(v)
     c.check(c.prefill() if T > 1 else c.decode(), f"values near 2^{power}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[70, 70, 70], [3000, 3000, 3000]])
+def test_an_exponent_byte_of_255_is_nan_whatever_its_codes(D, lens):
+    """Records from elsewhere may keep codes beside the mark: a value block's
+    channels become NaN, a key block makes its whole row so, and nothing else
+    changes; read_rows says the same."""
+    say(f"exponent byte 255, D={D}, {lens}")
+    c = Case(True, 4, 1, D, lens, (lens[0] + 63) // 32 * 32, 92)
+    clean = c.decode()
+    at = lens[0] - 9
+    *_, ke, ve = serve_ref.places(D)
+    c.cache.data[1, 0, at // 32, int(ve[at % 32, 1])] = 255
+    c.cache.data[1, 1, at // 32, int(ke[at % 32, 0])] = 255
+    k, v = c.cache.read_rows(1, 1)
+    assert v[0, 0, at, 32:64].isnan().all() and k[0, 1, at, :32].isnan().all()
+    out = c.decode()
+    assert out[0][:, 32:64].isnan().all()
+    rest = [d for d in range(D) if not 32 <= d < 64]
+    assert torch.equal(out[0][:, rest], clean[0][:, rest])
+    assert out[1].isnan().all() and torch.equal(out[2], clean[2])
+    bf16 = c.decode(torch.bfloat16)
+    assert torch.equal(bf16.isnan(), out.isnan())
