@@ -109,6 +109,15 @@ __device__ __forceinline__ void group_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Between writes to LDS and reads of them by other lanes of the wave, and before
+// the place is written again: the hardware takes a wave's LDS operations in order,
+// and the compiler, which sees one lane's addresses only, must not change it.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // What one column (query row) attends: p <= n with p < sinks or p >= lo.
 struct Reach {
   int n, lo;
@@ -408,12 +417,14 @@ void window_kernel(WindowPrefillParams p) {
 #pragma unroll
     for (int db = 0; db < DB; ++db)
       *staged_chunk<D>(staged, w.col, db * 4 + w.grp) = st[c].acc[db] * inv;
+    wave_lds_fence();
     if (p.out_bf16)
       store_rows<D, true>(p, staged, rows - (row0 + 16 * c), lane,
                           [&](int row) { return offset_of(row0 + 16 * c + row); });
     else
       store_rows<D, false>(p, staged, rows - (row0 + 16 * c), lane,
                            [&](int row) { return offset_of(row0 + 16 * c + row); });
+    wave_lds_fence();
   }
 }
 
