@@ -610,7 +610,8 @@ class QCache:
         n, T = k_rows.shape[0], k_rows.shape[2]
         device, at, shape = self._rows(starts, n, T)
         _check(lib().mlkv_qcache_write_rows(
-            self.struct, kv_begin, n, at, T, _arg(k_rows, shape, torch.bfloat16, device, "k_rows"),
+            self.struct, *_counts(kv_begin, n), at, *_counts(T),
+            _arg(k_rows, shape, torch.bfloat16, device, "k_rows"),
             _arg(v_rows, shape, torch.bfloat16, device, "v_rows"),
             _call_stream(stream, device, k_rows, v_rows, starts)))
 
@@ -623,8 +624,8 @@ class QCache:
         device, at, shape = self._rows(starts, n, T)
         k, v = torch.empty((2, *shape), dtype=torch.bfloat16, device=self.data.device).unbind()
         _write_on(stream, (k,), lambda handle: _check(lib().mlkv_qcache_read_rows(
-            self.struct, kv_begin, n, at, T, k.data_ptr(), v.data_ptr(), handle)),
-            device)
+            self.struct, *_counts(kv_begin, n), at, *_counts(T), k.data_ptr(), v.data_ptr(),
+            handle)), device)
         return k, v
 
 
@@ -668,8 +669,8 @@ def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, ma
     device = _launch_device(cache._device)
     shape = (cache.batch, map_._heads, cache.head_dim)
     ws_ptr, ws_bytes = _ws_args(ws, device)
-    if (window | sinks | max_len_hint) >> 31:  # some negative or beyond a C int
-        window, sinks, max_len_hint = _counts(window, sinks, max_len_hint)
+    if (layer | window | sinks | max_len_hint) >> 31:  # some negative or beyond a C int
+        layer, window, sinks, max_len_hint = _counts(layer, window, sinks, max_len_hint)
     _check(f(layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_._h,
              _arg(seq_lens, (shape[0],), torch.int32, device, "seq_lens"), window, sinks,
              _arg(out, shape, out.dtype, device, "out"), _out_dtype(out), max_len_hint, ws_ptr,
@@ -703,8 +704,8 @@ def prefill_attention_window(layer: int, q: torch.Tensor, cache: Cache, map_: Ma
     (fp32 or bf16); token t of sequence b stands at position ctx_lens[b] + t."""
     device = _launch_device(cache._device)
     shape = (cache.batch, q.shape[1], map_._heads, cache.head_dim)
-    if (window | sinks) >> 31:
-        window, sinks = _counts(window, sinks)
+    if (layer | window | sinks) >> 31:
+        layer, window, sinks = _counts(layer, window, sinks)
     _check(lib().mlkv_prefill_attention_window(
         layer, _arg(q, shape, torch.bfloat16, device, "q"), cache.struct, map_.handle,
         _arg(ctx_lens, shape[:1], torch.int32, device, "ctx_lens"), shape[1], window, sinks,
@@ -733,6 +734,8 @@ def norm_rope_append(layer: int, map_: Map, cache, q: torch.Tensor, k_new: torch
         if k_new is None or v_new is None:
             raise ValueError(f"layer {layer} owns KV heads: k_new and v_new are needed")
         kp, vp, stride = _new_rows(layer, map_, cache, k_new, v_new, T, device)
+    if rotary_dims >> 31:
+        rotary_dims = next(_counts(rotary_dims))
     nr = _NormRope(
         None if q_norm is None else _arg(q_norm, (D,), torch.bfloat16, device, "q_norm"),
         None if k_norm is None else _arg(k_norm, (D,), torch.bfloat16, device, "k_norm"),

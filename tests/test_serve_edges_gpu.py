@@ -100,3 +100,31 @@ def test_an_exponent_byte_of_255_is_nan_whatever_its_codes(D, lens):
     assert out[1].isnan().all() and torch.equal(out[2], clean[2])
     bf16 = c.decode(torch.bfloat16)
     assert torch.equal(bf16.isnan(), out.isnan())
+
+
+@pytest.mark.parametrize("four_bits", [True, False])
+def test_layers_heads_and_dims_beyond_a_c_int_are_refused(four_bits):
+    """They would be another number as a C int, one that is allowed."""
+    say(f"numbers beyond a C int, four_bits={four_bits}")
+    c = Case(four_bits, 4, 1, 64, [40, 33], 64, 93)
+    before = (c.cache.data if four_bits else c.cache.k).clone()
+    q, out = c.q.view(2, 1, 4, 64), torch.empty_like(c.q)
+    new = torch.ones((2, 1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    rows = torch.ones((1, 2, 64, 64), dtype=torch.bfloat16, device="cuda")
+    for far in (2 ** 32, -2 ** 32):
+        calls = [lambda: mlkv.norm_rope_append(2, c.map, c.cache, q, new, new, c.seq_lens - 1,
+                                               out.view(2, 1, 4, 64), rotary_dims=16 + far)]
+        c.layer = 3 + far
+        calls.append(c.decode)
+        if four_bits:
+            calls += [lambda: c.cache.write_rows(rows, rows, 1 + far),
+                      lambda: c.cache.read_rows(1 + far, 1),
+                      lambda: c.cache.read_rows(1, 0, T=5 + 2 ** 32)]
+        else:
+            calls.append(lambda: mlkv.prefill_attention_window(
+                3 + far, q, c.cache, c.map, c.seq_lens - 1, out.view(2, 1, 4, 64), 8))
+        for call in calls:
+            with pytest.raises(mlkv.MLKVError):
+                call()
+    assert torch.equal(before.view(torch.uint8),
+                       (c.cache.data if four_bits else c.cache.k).view(torch.uint8))
