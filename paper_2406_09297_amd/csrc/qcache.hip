@@ -115,8 +115,9 @@ __device__ __forceinline__ int angle_place(int pair, int half) {
 // then rotated with the angles at cs (those of the row's token) of the lane's
 // pairs, in fp32, rounded once to bf16.  All D / 8 lanes of a row take part.
 template <int D>
-__device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, float eps,
-                                             const float2* cs, int half) {
+__device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, const StoreParams& p,
+                                             const float2* cs) {
+  const int half = p.half;
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(raw[i]);
@@ -124,18 +125,19 @@ __device__ __forceinline__ u16x8 norm_rotate(const Lane<D>& ln, u16x8 raw, float
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    float mean = row_sum<D>(ss) * (1.f / D) + eps;
-    // Squares that leave fp32 at either end: the same row times a power of two
-    // (the quotient does not change).  A row's lanes take one side together.
+    float mean = row_sum<D>(ss) * (1.f / D) + p.eps;
+    // Squares, or an eps, that leave fp32 at either end: the same row times a power
+    // of two (the quotient does not change).  A row's lanes take one side together.
     if (!(mean < INFINITY) || mean < 0x1p-90f) {
-      const float scale = mean < 1.f ? 0x1p80f : 0x1p-80f;
+      const bool up = mean < 1.f;
+      const float scale = up ? 0x1p80f : 0x1p-80f;
       ss = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] *= scale;
         ss = fmaf(x[i], x[i], ss);
       }
-      mean = row_sum<D>(ss) * (1.f / D) + eps * scale * scale;
+      mean = row_sum<D>(ss) * (1.f / D) + (up ? p.eps_up : p.eps_down);
     }
     const float inv = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
@@ -234,7 +236,7 @@ __device__ __forceinline__ void norm_queries(const StoreParams& p, unsigned item
     const unsigned row = r, t = tok, hd = head;
     r += ROWS;
     if (r0 + ROWS < end) request();
-    const u16x8 out = norm_rotate<D>(ln, x, p.eps, cs + (t - tok0) * p.half, p.half);
+    const u16x8 out = norm_rotate<D>(ln, x, p, cs + (t - tok0) * p.half);
     if (row < end)
       *reinterpret_cast<u16x8*>(p.q_out + (static_cast<size_t>(t) * p.h + hd) * D + ln.c0) = out;
   }
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(StoreParams p) {
   for (int pass = 0; pass < PASSES; ++pass) {
     const int u = pass * ROWS + row;
     u16x8 k = xk[pass];
-    if (NORM) k = norm_rotate<D>(ln, k, p.eps, cs + u * p.half, p.half);
+    if (NORM) k = norm_rotate<D>(ln, k, p, cs + u * p.half);
     if (Q4) {
       const int e = block_exp(block_top(k));
       if (u >= u_lo && u < u_end) {

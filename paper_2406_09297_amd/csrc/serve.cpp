@@ -332,6 +332,8 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
   p.half = nr->rotary_dims / 2;
   p.inv_half = p.half ? ((1u << 20) + p.half - 1) / p.half : 0;
   p.eps = static_cast<float>(nr->eps);
+  p.eps_up = static_cast<float>(nr->eps * 0x1p160);
+  p.eps_down = static_cast<float>(nr->eps * 0x1p-160);
   // Revolutions base^(-2j / dims) / 2 pi, as the product of two powers each
   // (sixteen powers instead of up to 64, 3 us of a call).
   for (int j = 0; j < 8 && j < p.half; ++j)

@@ -48,7 +48,7 @@ struct StoreParams {
   uint32_t inv_h;             // (2^32 - 1) / h
   int half;                   // rotated channel pairs (0: none)
   unsigned inv_half;          // 2^20 / half, rounded up
-  float eps;
+  float eps, eps_up, eps_down;  // eps, and times 2^160 and 2^-160 (from 64 bits)
   // A position turns pair j by coarse[j / 8] * fine[j % 8] revolutions (64
   // products in the arguments cost 0.4 us a launch).
   double coarse[kMaxRopePairs / 8], fine[8];

@@ -128,3 +128,28 @@ def test_layers_heads_and_dims_beyond_a_c_int_are_refused(four_bits):
                 call()
     assert torch.equal(before.view(torch.uint8),
                        (c.cache.data if four_bits else c.cache.k).view(torch.uint8))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("eps,powers", [(1e-50, (-80, -100, None, 0)), (1e-42, (-70, None, -100, 5)),
+                                        (1e39, (60, 100, 0, None)), (1e60, (100, 120, 20, None))])
+def test_norms_whose_eps_leaves_fp32(D, eps, powers):
+    """Rows of about 2^power (None: zeros, which stay zeros) beside an eps that
+    fp32 holds as a subnormal number, as 0 or as inf."""
+    say(f"norm with eps {eps}, D={D}")
+    h, B = 3, len(powers)
+    f = synth.bf16_to_f32(synth.normal_bf16(94, 0, (B, 1, h, D)))
+    f = np.where(np.abs(f) < 2.0 ** -6, np.float32(2.0 ** -6), f)
+    f = np.stack([np.zeros_like(x) if n is None else np.ldexp(x, n) for x, n in zip(f, powers)])
+    bits = synth.f32_to_bf16(f.astype(np.float32))
+    w = synth.f32_to_bf16((1 + 0.1 * synth.bf16_to_f32(synth.normal_bf16(94, 9, (D,)))))
+    mp = mlkv.Map.uniform(2, h, 1, 1)
+    cache = mlkv.Cache.empty(1, B, 32, D)
+    q_out = torch.empty((B, 1, h, D), dtype=torch.bfloat16, device="cuda")
+    ctx = np.arange(B, dtype=np.int32)
+    mlkv.norm_rope_append(1, mp, cache, mlkv.bf16_tensor(bits, "cuda"), None, None,
+                          torch.from_numpy(ctx).cuda(), q_out, q_norm=mlkv.bf16_tensor(w, "cuda"),
+                          eps=eps, rotary_dims=32)
+    ref, bound = serve_ref.norm_rope(bits, w, eps, 32, 10000.0, ctx[:, None])
+    d = np.abs(q_out.double().cpu().numpy() - ref)
+    assert np.all(d <= bound), [(n, float((d[i] - bound[i]).max())) for i, n in enumerate(powers)]
