@@ -478,7 +478,8 @@ size_t mlkv_workspace_bytes_window(const mlkv_map* map, int batch, int capacity,
 /* mlkv_prefill_attention within a window: token t of sequence b stands at
  * position n = ctx_lens[b] + t and attends the positions p <= n with p < sinks
  * or p > n - window (window and sinks as above; window 0: no limit).  Other
- * arguments, limits and errors as mlkv_prefill_attention. */
+ * arguments, limits and errors as mlkv_prefill_attention; with T = 0 the tensors
+ * are not looked at. */
 mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_cache* cache,
                                           const mlkv_map* map, const int32_t* ctx_lens, int T,
                                           int window, int sinks, void* out,

@@ -480,16 +480,16 @@ mlkv_status mlkv_prefill_attention_window(int layer, const void* q, const mlkv_c
   if (static_cast<long>(B) * map->kv_count[layer] >= mlkv::kMaxPrefillUnits)
     return fail(MLKV_ERR_UNSUPPORTED, "%ld (sequence, KV head) units: at most %ld",
                 static_cast<long>(B) * map->kv_count[layer], mlkv::kMaxPrefillUnits - 1);
+  if (out_dtype != MLKV_OUT_F32 && out_dtype != MLKV_OUT_BF16)
+    return fail(MLKV_ERR_INVALID_ARG, "bad out_dtype");
+  if (T == 0) return ok();
   if (!q || !ctx_lens || !out)
     return fail(MLKV_ERR_INVALID_ARG, "q, ctx_lens, out must be non-NULL");
   if (!aligned16(q) || !aligned16(out))
     return fail(MLKV_ERR_ALIGNMENT, "q and out must be 16-byte aligned");
   if (!aligned4(ctx_lens)) return fail(MLKV_ERR_ALIGNMENT, "ctx_lens must be 4-byte aligned");
-  if (out_dtype != MLKV_OUT_F32 && out_dtype != MLKV_OUT_BF16)
-    return fail(MLKV_ERR_INVALID_ARG, "bad out_dtype");
   if ((s = check_prefill_lengths_if_requested(ctx_lens, B, T, cache->capacity, stream)) != MLKV_OK)
     return s;
-  if (T == 0) return ok();
   mlkv::WindowPrefillParams p{};
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(cache->k);
