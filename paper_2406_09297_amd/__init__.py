@@ -399,11 +399,10 @@ def workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda"
     """Allocate and initialise (mlkv_workspace_init) a decode workspace (with
     room for the rotary table of mlkv_decode_step_rope when rotary_dims > 0)."""
     n = map_.workspace_bytes(batch, capacity, head_dim, rotary_dims)
-    return _initialised(n, device, stream)
+    return _initialised(torch.empty(max(n, 16), dtype=torch.uint8, device=device), stream)
 
 
-def _initialised(n: int, device, stream) -> torch.Tensor:
-    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+def _initialised(ws: torch.Tensor, stream) -> torch.Tensor:
     _write_on(stream, (ws,), lambda handle: _check(
         lib().mlkv_workspace_init(ws.data_ptr(), ws.numel(), handle)))
     return ws
@@ -659,9 +658,12 @@ def qcache_append_rows(layer: int, map_: Map, cache: QCache, k_new: torch.Tensor
 
 def window_workspace(map_: Map, batch: int, capacity: int, head_dim: int, device="cuda",
                      stream=None) -> torch.Tensor:
-    """Allocate and initialise a workspace of mlkv_workspace_bytes_window bytes."""
+    """Allocate and initialise a workspace of mlkv_workspace_bytes_window bytes on
+    the current device, whose size it is."""
     n = lib().mlkv_workspace_bytes_window(map_.handle, batch, capacity, head_dim)
-    return _initialised(n, device, stream)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    _launch_device(ws.get_device())
+    return _initialised(ws, stream)
 
 
 def _window_attention(f, layer, q, cache, map_, seq_lens, out, window, sinks, max_len_hint, ws,

@@ -74,10 +74,11 @@ MAKERS = [lambda s: _cache(mlkv.Cache).read_rows(stream=s),
 
 
 @pytest.mark.parametrize("make", MAKERS)
-def test_what_a_call_allocates_is_written_in_order(make, world):
+def test_what_a_call_allocates_is_written_in_order(make, world, monkeypatch):
     """Memory from the current stream's pool is written on another stream only
     behind the work that the current one was given, and the allocator is told
     (or, for a bare handle, the current stream waits) before it can be reused."""
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
     for stream in (None, world.current, CURRENT):
         world.log.clear()
         make(stream)
@@ -132,3 +133,12 @@ def test_a_call_on_another_stream_comes_after_its_tensors(n, world, monkeypatch)
     assert world.log == [("wait", SIDE, CURRENT)] + [("record", SIDE)] * kept + [("launch", SIDE)]
     with pytest.raises(ValueError, match="stream on device 1"):
         call(FakeStream(SIDE, world.log, device_index=1))
+
+
+def test_a_workspace_elsewhere_is_refused(world, monkeypatch):
+    """Its size is the current device's, and its fill would run there."""
+    for device in (-1, 1):
+        monkeypatch.setattr(torch.Tensor, "get_device", lambda t: device)
+        with pytest.raises(ValueError, match="not the current one"):
+            mlkv.window_workspace(MAP, 1, 32, 64, device="cpu")
+    assert ("launch", CURRENT) not in world.log
