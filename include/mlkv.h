@@ -373,8 +373,9 @@ mlkv_status mlkv_prefill_step(const void* q_all, const void* k_new_all, const vo
  * same memory, on top of what sharing the heads saves (Section 3).  A token's
  * key and value rows are held in blocks of 32 channels; a block's values are
  * 2^e times one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign.  e is the least for
- * which the block's largest magnitude is below 7 * 2^e, in [-124, 125]; each
- * value is rounded to the nearest, ties to the even code.  Every value held is
+ * which the block's largest magnitude is below 7 * 2^e, but at least -124 and at
+ * most 125; each value is rounded to the nearest, ties to the even code
+ * (magnitudes from 7 * 2^125 on become 6 * 2^125).  Every value held is
  * a bf16 number, and a row read back and stored again is held as before.  A
  * block with a value that is not finite is held as NaN throughout.
  *
@@ -410,7 +411,8 @@ size_t mlkv_qcache_bytes(const mlkv_map* map, int batch, int capacity, int head_
 /* mlkv_cache_append_rows for the 4-bit cache: the T new rows (a decode step's
  * newest token: T = 1) of the KV heads `layer` owns at slots ctx_lens[b] + t.
  * Same arguments and errors; slots outside [0, capacity) are skipped, and
- * nothing but the rows' slots changes. */
+ * nothing but the rows' slots changes.  Tokens share bytes: calls that store into
+ * one sequence of a KV head must be ordered, also on slots of their own. */
 mlkv_status mlkv_qcache_append_rows(int layer, const mlkv_map* map, const mlkv_qcache* cache,
                                     const void* k_new, const void* v_new, int T,
                                     int new_row_stride, const int32_t* ctx_lens,

@@ -40,7 +40,8 @@ __device__ __forceinline__ float exp_scale(uint32_t byte) {
 // The exponent byte of a block whose largest magnitude has bf16 pattern `top`:
 // the least 2^e with top < 7 2^e (adding a quarter of a binade carries where
 // the magnitude passes 1.75 of its power of two), so that the largest value
-// becomes 4 or 6 steps and none is more than half a step of its place off.
+// becomes 4 or 6 steps and none is more than half a step of its place off, save
+// those from 7 2^125 on, which become 6 steps of 2^125.
 __device__ __forceinline__ int block_exp(int top) {
   if (top >= 0x7F80) return kQNaN;
   const int e = ((top + 0x20) >> 7) - 2;

@@ -13,8 +13,9 @@
 //
 // A block of 32 channels with largest magnitude a is held as codes c of e2m1
 // (+-0, 0.5, 1, 1.5, 2, 3, 4, 6) times 2^e, e the least with a < 7 2^e: the top
-// code's rounding range ends there, so nothing saturates and each value is the
-// nearest that its scale can hold.  A row x of a query or key becomes
+// code's rounding range ends there, so each value is the nearest that its scale
+// can hold and none saturates below 7 2^125; from there on (bf16's last eighth of
+// a binade) values are held as 6 2^125, as 4 2^126 is no bf16 number.  A row x of a query or key becomes
 // y = w x / sqrt(mean(x^2) + eps), its pairs (j, j + half) turned by pos
 // times the pair's angle, in fp32 and rounded once.
 //

@@ -140,9 +140,10 @@ mlkv_status check_row_buffers(const void* k_rows, const void* v_rows) {
 // kSpanLongTiles tiles (us, cut / not, 4 bits: 300 units of 4000 .. 32000 tokens
 // 81 / 129, 140 of 8000 .. 16000 30 / 43, 264 of 8000 34 / 45, 320 of 16000 with
 // 128 channels 125 / 134; bf16, 288 windows of 4096 114 / 134; from 16 tiles on
-// instead, 384 bf16 windows of 1023 take 45.6 for 41.9).  Fewer bf16
-// units than compute units stay whole: they reach the memory's rate as they are
-// (160 windows of 4096: 68 / 63).  Grids of more workgroups than compute units
+// instead, 384 bf16 windows of 1023 take 45.6 for 41.9).  bf16 units that are no
+// more than the compute units take only the first cut, into cus / units runs: those
+// that it leaves whole reach the memory's rate as they are (160 windows of 4096
+// cut / not: 68 / 63).  Grids of more workgroups than compute units
 // take four waves, of which more are resident at once (48 x 8 windows of 1023,
 // 128 channels, bf16 43.8 / 45.3).
 struct SpanPlan {
