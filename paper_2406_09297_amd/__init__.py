@@ -191,14 +191,10 @@ def _write_on(stream, made, call, device: int | None = None):
     still does with former tensors there, and before it goes to others."""
     if stream is None:
         return call(_stream(None, device))
+    if isinstance(stream, torch.cuda.Stream):
+        return call(_call_stream(stream, made[0].get_device(), *made))
     at = made[0].device
     current = torch.cuda.current_stream(at)
-    if isinstance(stream, torch.cuda.Stream):
-        if stream != current:
-            stream.wait_stream(current)
-            for t in made:
-                t.record_stream(stream)
-        return call(stream.cuda_stream)
     # A bare handle's stream may be gone before the tensors are: the current
     # stream waits for it instead of the allocator.
     if int(stream) == current.cuda_stream:

@@ -88,6 +88,8 @@ def test_what_a_call_allocates_is_written_in_order(make, world, monkeypatch):
     made = world.log.count(("empty",))
     assert world.log[:made + 1] == [("empty",)] * made + [("wait", SIDE, CURRENT)]
     assert sorted(world.log[made + 1:]) == [("launch", SIDE)] + [("record", SIDE)] * made
+    with pytest.raises(ValueError, match="stream on device 1"):
+        make(FakeStream(SIDE, world.log, device_index=1))
     for handle in (SIDE, 0):  # 0: the default stream
         world.log.clear()
         make(handle)
