@@ -3,6 +3,7 @@
 // error is reported before any HIP call.
 #include "mlkv.h"
 
+#include <cfloat>
 #include <cmath>
 
 #include "host.h"
@@ -265,6 +266,9 @@ mlkv_status span_attention(int layer, const void* q, const mlkv_cache* bf16, con
   return ok();
 }
 
+// A number not below 0 as fp32, inf where fp32 ends (a cast alone is undefined there).
+float to_float(double x) { return x > FLT_MAX ? HUGE_VALF : static_cast<float>(x); }
+
 // Passes of a query workgroup (below; us, 16000 tokens of 12 and 4 heads of 64
 // channels, all turned, with 8 / 4 / 16 workgroups a compute unit 18.2 / 19.5 /
 // 18.7; 8000 of 32 and 8 heads of 128 with at most 4 / 8 passes 45.8 / 47.5).
@@ -332,9 +336,9 @@ mlkv_status norm_rope_append(int layer, const mlkv_map* map, const mlkv_cache* b
   p.inv_h = 0xFFFFFFFFu / static_cast<uint32_t>(h);
   p.half = nr->rotary_dims / 2;
   p.inv_half = p.half ? ((1u << 20) + p.half - 1) / p.half : 0;
-  p.eps = static_cast<float>(nr->eps);
-  p.eps_up = static_cast<float>(nr->eps * 0x1p160);
-  p.eps_down = static_cast<float>(nr->eps * 0x1p-160);
+  p.eps = to_float(nr->eps);
+  p.eps_up = to_float(nr->eps * 0x1p160);
+  p.eps_down = to_float(nr->eps * 0x1p-160);
   // Revolutions base^(-2j / dims) / 2 pi, as the product of two powers each
   // (sixteen powers instead of up to 64, 3 us of a call).
   for (int j = 0; j < 8 && j < p.half; ++j)
